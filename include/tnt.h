@@ -368,8 +368,8 @@ tnt_status tnt_delta_step(const tnt_delta_config* cfg, const tnt_delta_strides* 
  *    every step.  They must keep the singular values that start in [0, 1] at or below 4
  *    and b A + c A^2 at or below 64 in norm (TNT_ERR_ARG): the products hold their
  *    operands in 16 bits at fixed scales.
- *  - fp32 matrices are computed to fp32 accuracy; bf16 ones with intermediate products
- *    of 11-bit operands and rounded once.
+ *  - Everything is computed to fp32 accuracy, whatever the matrices' type and sizes;
+ *    outputs are rounded once.
  *  - A zero matrix gives zeros (eps > 0); a NaN or infinite entry spoils its own matrix
  *    alone.  Any sizes from 1 to 32768, any alignment of rows; out may be G. */
 typedef struct {

@@ -9,6 +9,7 @@ namespace tnt {
 
 constexpr int ORTH_MAX_STEPS = 16;
 constexpr int ORTH_PART = 256;  // partial sums of a matrix's norm, at most
+constexpr int ORTH_TILE = 64;   // sides of the tiles of the products of large matrices
 
 struct OrthArgs {
   const void* G;
@@ -35,9 +36,6 @@ struct OrthArgs {
 
 // one workgroup a matrix: fits its registers
 bool orth_small(int m, int k);
-// large form: tile sides that its products take
-int orth_tile_sym(int n, int m);
-int orth_tile_update(int n, int m, int k, bool bf16);
 hipError_t launch_orth_small(const OrthArgs& a, hipStream_t st);
 hipError_t launch_orth_large(const OrthArgs& a, hipStream_t st);
 

@@ -8,10 +8,9 @@
 //     hi hi + hi lo + lo hi
 // reach the accuracy of fp32 arithmetic at 3 MFMAs (measured against 64 bits: 7e-7 to
 // 2e-6 on 64 x 256 to 512 x 512, fp32 itself 1.3e-6 to 2.2e-6; bf16 terms need 6
-// products for that, and with 3 are 20 to 40 times worse).  For bf16 updates the two
-// products with X take hi hi alone: the result is rounded to 8 bits anyway, and they
-// add 1.1e-3 to 1.7e-3 to that rounding's 1.7e-3; A^2 keeps its three, since b A + c A^2
-// cancels (with one: 2.5e-3 to 3e-3).
+// products for that, and with 3 are 20 to 40 times worse).  bf16 updates are computed the
+// same way and rounded once: one term in the products with X would halve the time of a
+// 4096 x 2048 one, but add 1e-3 to 1.7e-3 to that rounding's 1.7e-3.
 #include "tnt_orth.h"
 
 #include "tnt_device.h"
@@ -388,10 +387,13 @@ __global__ __launch_bounds__(256) void orth_scale_kernel(OrthArgs a) {
 
 // ---------------------------------------------------------------------------------
 // C = P Q^T, both with the contraction along the rows of memory, TM x TM a workgroup of
-// four waves (2 x 2).  Steps of 32: the planes' rows go straight from global memory to
-// LDS (16 bytes a lane, 64-byte rows, the 16-byte pieces of a row permuted by the row so
+// four waves (2 x 2).  Steps of 64: the planes' rows go straight from global memory to
+// LDS (16 bytes a lane, 128-byte rows, the 16-byte pieces of a row permuted by the row so
 // that a wave's fragment reads meet no bank twice), the next step's while this one is
-// multiplied.
+// multiplied.  Tiles of 64, two workgroups a CU: of 128, one a CU, GRAM and SQUARE are slower
+// at every size (five steps with those of 4096 x 2048 so: 1.50 ms against 1.41; 64 matrices of
+// 510 x 500: 1.23 / 1.12); UPDATE is 3 to 9 % faster from 1024 rows on (4096 x 2048: 1.37)
+// and up to a fifth slower below (16 of 520 x 510: 0.43 / 0.36).
 //   GRAM    A = X X^T           lower tiles, written both ways round
 //   SQUARE  B = b A + c A A     lower tiles, written both ways round
 //   UPDATE  X^T <- a X^T + X^T B, both orientations (X in place: a tile reads its own
@@ -403,15 +405,17 @@ enum { GRAM = 0, SQUARE = 1, UPDATE = 2, LAST = 3 };
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
 
-template <int N> __device__ __forceinline__ void wait_loads() {
-  static_assert(N >= 0 && N < 64, "vmcnt has six bits");
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+// every load into LDS has arrived, and every wave is done reading what the next one overwrites
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-template <int TM, int NPROD, int EPI, int BK, int NS>
+constexpr int TM = ORTH_TILE, BK = 64;  // sides of a tile; contraction elements a stage
+
+template <int EPI>
 __global__ __launch_bounds__(256) void orth_gemm_kernel(OrthArgs a, int step, int tiles, int share) {
-  constexpr int NPL = NPROD == 1 ? 1 : 2, WT = TM / 32;  // planes; 16-row tiles a wave and side
-  constexpr int SIDE = TM * BK, STAGE = 2 * NPL * SIDE;  // elements a plane and side; a stage
+  constexpr int WT = TM / 32;                      // 16-row tiles a wave and side
+  constexpr int SIDE = TM * BK, STAGE = 4 * SIDE;  // elements a plane and side; a stage
   extern __shared__ __attribute__((aligned(16))) _Float16 sh[];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q = lane >> 4, c = lane & 15;
@@ -439,12 +443,12 @@ __global__ __launch_bounds__(256) void orth_gemm_kernel(OrthArgs a, int step, in
   const size_t pp = EPI == SQUARE ? pa : EPI == GRAM ? px : pt, pq = EPI == GRAM ? px : pa;
   const int ld = EPI == GRAM ? a.lk : a.lm, nk = (EPI == GRAM ? a.kp : a.mp) / BK;
   // loads: a wave brings 1 KB, RR rows of BK, a request
-  constexpr int PC = BK / 8, RR = 64 / PC, REQ = 2 * NPL * TM / RR, PER = REQ / 4;
-  const int lrow = lane / PC, piece = (lane % PC) ^ (BK == 64 ? lrow & 7 : (lrow >> 1) & 3);
+  constexpr int PC = BK / 8, RR = 64 / PC, REQ = 4 * TM / RR, PER = REQ / 4;
+  const int lrow = lane / PC, piece = (lane % PC) ^ (lrow & 7);
   const _Float16* src[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int r = w * PER + i, side = r / (NPL * TM / RR), rem = r - side * (NPL * TM / RR);
+    const int r = w * PER + i, side = r / (2 * TM / RR), rem = r - side * (2 * TM / RR);
     const int pl = rem / (TM / RR), rr = rem - pl * (TM / RR);
     src[i] = (side ? Q + pl * pq : P + pl * pp) +
              (size_t)((side ? tj : ti) * TM + RR * rr + lrow) * ld + 8 * piece;
@@ -461,38 +465,33 @@ __global__ __launch_bounds__(256) void orth_gemm_kernel(OrthArgs a, int step, in
 #pragma unroll
     for (int j = 0; j < WT; ++j) acc[i][j] = zero4();
   const int wi = (w >> 1) * (TM / 2), wj = (w & 1) * (TM / 2);
-  // NS - 1 stages on the way; past the last step the requests repeat it, so that the
-  // number outstanding is the same in every step
-#pragma unroll
-  for (int s = 0; s < NS - 1; ++s) fetch(s, min(s, nk - 1));
-  for (int ks = 0, st = 0; ks < nk; ++ks, st = st + 1 == NS ? 0 : st + 1) {
-    wait_loads<PER * (NS - 2)>();
-    fetch(st == 0 ? NS - 1 : st - 1, min(ks + NS - 1, nk - 1));
-    const _Float16* sp = sh + st * STAGE;
+  fetch(0, 0);
+  for (int ks = 0; ks < nk; ++ks) {
+    wait_loads();
+    fetch((ks + 1) & 1, min(ks + 1, nk - 1));  // (past the last step: again, into the stage not read)
+    const _Float16* sp = sh + (ks & 1) * STAGE;
 #pragma unroll
     for (int kk = 0; kk < BK / 32; ++kk) {
-      const int frag = c * BK + 8 * ((4 * kk + q) ^ (BK == 64 ? c & 7 : (c >> 1) & 3));
-      h8 pf[WT][NPL], qf[WT][NPL];
+      const int frag = c * BK + 8 * ((4 * kk + q) ^ (c & 7));
+      h8 pf[WT][2], qf[WT][2];
 #pragma unroll
       for (int i = 0; i < WT; ++i)
 #pragma unroll
-        for (int p = 0; p < NPL; ++p) {
+        for (int p = 0; p < 2; ++p) {
           pf[i][p] = *reinterpret_cast<const h8*>(sp + p * SIDE + (wi + 16 * i) * BK + frag);
-          qf[i][p] = *reinterpret_cast<const h8*>(sp + (NPL + p) * SIDE + (wj + 16 * i) * BK + frag);
+          qf[i][p] = *reinterpret_cast<const h8*>(sp + (2 + p) * SIDE + (wj + 16 * i) * BK + frag);
         }
 #pragma unroll
       for (int i = 0; i < WT; ++i)
 #pragma unroll
         for (int j = 0; j < WT; ++j) {
-          if (NPROD == 3) {
-            acc[i][j] = mma(pf[i][NPL - 1], qf[j][0], acc[i][j]);
-            acc[i][j] = mma(pf[i][0], qf[j][NPL - 1], acc[i][j]);
-          }
+          acc[i][j] = mma(pf[i][1], qf[j][0], acc[i][j]);
+          acc[i][j] = mma(pf[i][0], qf[j][1], acc[i][j]);
           acc[i][j] = mma(pf[i][0], qf[j][0], acc[i][j]);
         }
     }
   }
-  wait_loads<0>();  // no request is on its way into LDS, and every wave is done reading it
+  wait_loads();
   // The tile through LDS: both orientations leave in 16-byte stores of whole rows, by loops
   // over rows instead of code for every accumulator (with that, 20 us of a launch whose
   // products take 5 went to fetching its instructions).
@@ -576,33 +575,12 @@ __global__ __launch_bounds__(256) void orth_gemm_kernel(OrthArgs a, int step, in
   }
 }
 
-template <int TM, int NPROD, int EPI, int BK, int NS>
-void gemm(const OrthArgs& a, int step, hipStream_t st) {
-  constexpr size_t stages = (size_t)NS * 2 * (NPROD == 1 ? 1 : 2) * TM * BK * 2, tile = (size_t)TM * (TM + 1) * 4;
+template <int EPI> void gemm(const OrthArgs& a, int step, hipStream_t st) {
+  constexpr size_t stages = (size_t)2 * 4 * TM * BK * 2, tile = (size_t)TM * (TM + 1) * 4;
   constexpr size_t lds = stages > tile ? stages : tile;
   const int tm = a.mp / TM, tiles = EPI <= SQUARE ? tm * (tm + 1) / 2 : (a.kp / TM) * tm;
   const int share = (a.n * tiles + 7) / 8;
-  orth_gemm_kernel<TM, NPROD, EPI, BK, NS><<<8 * share, 256, lds, st>>>(a, step, tiles, share);
-}
-
-// Tiles of 64 where tiles of 128 would not give every CU its own (two, for the products
-// of lower tiles): m 2048, k 4096 in bf16, a step's GRAM 37 us against 55, SQUARE 52 / 63;
-// UPDATE, with 512 tiles of 128, 68 / 52.  With three products tiles of 64 hold their own
-// there too (m 2048, k 4096: all five steps 1.38 ms against 1.46; 55 matrices of 473 x 378,
-// which pad further to 128: 0.57 against 0.66).  More stages than these gained nothing.
-template <int NX> void steps_of(const OrthArgs& a, hipStream_t st) {
-  const bool sym = orth_tile_sym(a.n, a.m) == 128, upd = orth_tile_update(a.n, a.m, a.k, NX == 1) == 128;
-  for (int s = 0; s < a.steps; ++s) {
-    if (sym) {
-      gemm<128, NX, GRAM, 64, 2>(a, s, st);
-      gemm<128, 3, SQUARE, 64, 2>(a, s, st);
-    } else {
-      gemm<64, NX, GRAM, 64, NX == 1 ? 3 : 2>(a, s, st);
-      gemm<64, 3, SQUARE, 64, 2>(a, s, st);
-    }
-    if (s + 1 < a.steps) upd ? gemm<128, NX, UPDATE, 64, 2>(a, s, st) : gemm<64, NX, UPDATE, 64, 2>(a, s, st);
-    else upd ? gemm<128, NX, LAST, 64, 2>(a, s, st) : gemm<64, NX, LAST, 64, 2>(a, s, st);
-  }
+  orth_gemm_kernel<EPI><<<8 * share, 256, lds, st>>>(a, step, tiles, share);
 }
 
 template <int MT, int RP>
@@ -617,14 +595,6 @@ hipError_t small(const OrthArgs& a, hipStream_t st) {
 // CU a matrix is then the slower form: 32 matrices of 128 x 512 in 212 us.
 bool orth_small(int m, int k) { return m <= 64 && k <= 1024; }
 
-int orth_tile_sym(int n, int m) {
-  const int64_t t = (m + 127) / 128;
-  return n * t * (t + 1) / 2 >= 512 ? 128 : 64;
-}
-int orth_tile_update(int n, int m, int k, bool bf16) {
-  return bf16 && (int64_t)n * ((m + 127) / 128) * ((k + 127) / 128) >= 256 ? 128 : 64;
-}
-
 hipError_t launch_orth_small(const OrthArgs& a, hipStream_t st) {
   const int rp = a.k <= 256 ? 1 : a.k <= 512 ? 2 : 4;
   if (a.m <= 32) return rp == 1 ? small<2, 1>(a, st) : rp == 2 ? small<2, 2>(a, st) : small<2, 4>(a, st);
@@ -634,8 +604,12 @@ hipError_t launch_orth_small(const OrthArgs& a, hipStream_t st) {
 hipError_t launch_orth_large(const OrthArgs& a, hipStream_t st) {
   orth_norm_kernel<<<a.n * a.parts, 256, 0, st>>>(a);
   orth_scale_kernel<<<dim3(a.kp / 64, a.mp / 64, a.n), 256, 0, st>>>(a);
-  if (a.bf16) steps_of<1>(a, st);
-  else steps_of<3>(a, st);
+  for (int s = 0; s < a.steps; ++s) {
+    gemm<GRAM>(a, s, st);
+    gemm<SQUARE>(a, s, st);
+    if (s + 1 < a.steps) gemm<UPDATE>(a, s, st);
+    else gemm<LAST>(a, s, st);
+  }
   return hipGetLastError();
 }
 

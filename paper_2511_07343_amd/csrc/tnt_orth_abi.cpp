@@ -68,9 +68,8 @@ Lay lay_of(const tnt_orth_config* c) {
   const int64_t apart = std::max(std::max(c->g_row, c->out_row), (int64_t)c->cols);
   l.small = orth_small(l.m, l.k) && apart < INT32_MAX / 1024;
   if (l.small) return l;
-  const int t = std::max(orth_tile_sym(c->n, l.m), orth_tile_update(c->n, l.m, l.k, c->dtype == TNT_BF16));
-  l.mp = (l.m + t - 1) / t * t;
-  l.kp = (l.k + t - 1) / t * t;
+  l.mp = (l.m + ORTH_TILE - 1) / ORTH_TILE * ORTH_TILE;
+  l.kp = (l.k + ORTH_TILE - 1) / ORTH_TILE * ORTH_TILE;
   l.lm = l.mp + 64;
   l.lk = l.kp + 64;
   const size_t x = up256((size_t)c->n * 2 * l.mp * l.lk * 2), xt = up256((size_t)c->n * 2 * l.kp * l.lm * 2),

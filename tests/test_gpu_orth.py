@@ -165,3 +165,16 @@ def test_batch_of_initial_weights():
 def test_no_matrices():
     cfg = tnt.OrthConfig(n=0, rows=8, cols=8)
     assert tnt.orthogonalise(cfg, torch.empty(0, 8, 8, device=DEV)).shape == (0, 8, 8)
+
+
+@pytest.mark.parametrize("n,r,c", [(2, 64, 250), (1, 64, 1024), (1, 64, 1025), (2, 130, 200), (2, 300, 257),
+                                   (1, 512, 128), (1, 1030, 700)])
+def test_bf16_is_the_result_rounded_once(n, r, c):
+    """In both forms.  With an error e of the norm before it (the fp32 bound), a rounding goes the other
+    way for a part e / ulp of the elements, by an ulp: sqrt(e * ulp) of the norm, ulp at most 2^-7."""
+    G = matrices(n, r, c, torch.bfloat16, seed=r)
+    out = run(G.to(DEV)).double().cpu()
+    for i in range(n):
+        want = O.orthogonalise(G[i], [MUON] * 5).to(torch.bfloat16).double()
+        e = ((out[i] - want).norm() / want.norm()).item()
+        assert check_err(f"orth rounded {n}x{r}x{c}", f"out[{i}]", e, (1e-4 * 2.0 ** -7) ** 0.5), (i, e)
