@@ -596,7 +596,7 @@ def tnt_orth_update(c, coef, G, out, workspace, ws_bytes=None, stream=None) -> i
 def orthogonalise(cfg: OrthConfig, G: torch.Tensor, out: Optional[torch.Tensor] = None,
                   workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Run tnt_orth_update on G [n][rows][cols] (rows or columns of adjacent elements, any other
-    strides); returns ``out``, by default a new tensor laid out as G."""
+    strides but those of broadcasts); returns ``out``, by default a new tensor laid out as G."""
     _check(G, "G", (cfg.n, cfg.rows, cfg.cols), cfg.io, G.device)
     if out is None:
         out = torch.empty_like(G)
@@ -604,6 +604,9 @@ def orthogonalise(cfg: OrthConfig, G: torch.Tensor, out: Optional[torch.Tensor] 
         _check(out, "out", (cfg.n, cfg.rows, cfg.cols), cfg.io, G.device)
     c, flip = cfg.c, False
     if not (G.is_contiguous() and out.is_contiguous()):
+        for name, t in (("G", G), ("out", out)):  # to the library a stride of 0 is a contiguous tensor's
+            if any(t.shape[d] > 1 and t.stride(d) == 0 for d in range(3)):
+                raise ValueError(f"{name}: broadcast matrices, rows or columns")
         unit = lambda t, d: t.shape[d] == 1 or t.stride(d) == 1
         flip = not (unit(G, 2) and unit(out, 2))
         if flip and not (unit(G, 1) and unit(out, 1)):
@@ -613,8 +616,6 @@ def orthogonalise(cfg: OrthConfig, G: torch.Tensor, out: Optional[torch.Tensor] 
         row = lambda t: t.stride(r) if t.shape[r] > 1 else side
         c = tnt_orth_config(base.n, base.rows, base.cols, base.steps, base.dtype, base.eps, base.scale,
                             G.stride(0), row(G), out.stride(0), row(out))
-        if cfg.n > 1 and (G.stride(0) == 0 or row(G) == 0):
-            raise ValueError("G: broadcast matrices or rows")
     if workspace is None:
         workspace = _bytes(cfg.size, G.device)
     s = tnt_orth_update(c, cfg.coef, G, out, workspace, stream=_stream_of(G.device, stream))

@@ -78,3 +78,17 @@ def test_oracle_against_svd():
         for a, b, c in coef:
             s = a * s + b * s ** 3 + c * s ** 5
         assert (O.orthogonalise(G, coef) - (U * s) @ V).norm() <= 1e-10
+
+
+@pytest.mark.parametrize("shape,stride0", [((1, 1, 6), 1), ((1, 4, 1), 2), ((2, 1, 6), 1), ((2, 4, 1), 2), ((1, 4, 6), 0)])
+def test_broadcast_extents_are_refused(shape, stride0):
+    """A stride of 0 means "contiguous" to the library: a broadcast row, column or matrix would be
+    read, or written, past its memory.  One matrix too, and `out` as well as G."""
+    n = 2 if stride0 == 0 else shape[0]
+    cfg = tnt.OrthConfig(n=n, rows=4, cols=6)
+    wide, whole = torch.zeros(shape).expand(n, 4, 6), torch.zeros(n, 4, 6)
+    assert wide.stride(stride0) == 0
+    with pytest.raises(ValueError, match="G: broadcast"):
+        tnt.orthogonalise(cfg, wide)
+    with pytest.raises(ValueError, match="out: broadcast"):
+        tnt.orthogonalise(cfg, whole, out=wide)
