@@ -464,11 +464,27 @@ def _delta_inputs(cfg: DeltaConfig, x):
     return dev, st
 
 
-def _stream_of(dev, stream):
-    """The given stream, or the current one of the tensors' device."""
-    if stream is not None or dev.type != "cuda":
-        return stream
-    return torch._C._cuda_getCurrentRawStream(dev.index)
+def _current(dev):
+    """The current stream of the tensors' device."""
+    return torch._C._cuda_getCurrentRawStream(dev.index) if dev.type == "cuda" else None
+
+
+def _on_stream(stream, dev, inputs, call):
+    """``call()`` with ``stream`` (torch's, or a handle) as the current one: what it allocates is
+    that stream's, so that a buffer dropped on return is given to nothing that does not wait for the
+    kernels using it.  The inputs are marked as used there, the outputs as used on the caller's
+    stream.  Ordering the two streams is the caller's, as with any torch work on a side stream."""
+    back = torch.cuda.current_stream(dev)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(stream, device=dev)
+    with torch.cuda.stream(stream):
+        out = call()
+    made = out.values() if isinstance(out, dict) else out if isinstance(out, tuple) else (out,)
+    for tensors, s in ((inputs, stream), (made, back)):
+        for t in tensors:
+            if t is not None:
+                t.record_stream(s)
+    return out
 
 
 def _delta_rest(cfg: DeltaConfig, x, dev):
@@ -487,6 +503,9 @@ def delta_forward(cfg: DeltaConfig, x: Dict[str, torch.Tensor], save: bool = Tru
                   stream=None):
     """Run tnt_delta_fwd on ``x`` (q, k, v, g, lr and, where given, S0 and seq_start; any strides
     with adjacent elements); returns (o in v's layout, saved or None, final state or None)."""
+    if stream is not None and x["q"].is_cuda:
+        return _on_stream(stream, x["q"].device, (*x.values(), workspace),
+                          lambda: delta_forward(cfg, x, save, final_state, workspace))
     dev, st = _delta_inputs(cfg, x)
     S0, start = _delta_rest(cfg, x, dev)
     o = torch.empty_like(x["v"])
@@ -497,7 +516,7 @@ def delta_forward(cfg: DeltaConfig, x: Dict[str, torch.Tensor], save: bool = Tru
     if workspace is None:
         workspace = _bytes(cfg.size(TNT_WS_FWD), dev)
     s = tnt_delta_fwd(cfg, _delta_strides6(*st), x["q"], x["k"], x["v"], x["g"], x["lr"], start,
-                      S0, o, fin, saved, workspace, stream=_stream_of(dev, stream))
+                      S0, o, fin, saved, workspace, stream=_current(dev))
     if s != 0:
         raise TntError(s, "tnt_delta_fwd")
     return o, saved, fin
@@ -508,6 +527,9 @@ def delta_backward(cfg: DeltaConfig, x: Dict[str, torch.Tensor], dO: torch.Tenso
                    workspace: Optional[torch.Tensor] = None, stream=None):
     """Run tnt_delta_bwd; returns the gradients of sum(dO * o) + sum(dfinal * final state) in
     their inputs' layouts (dS0 where there is an S0).  ``saved`` None: recomputed."""
+    if stream is not None and x["q"].is_cuda:
+        return _on_stream(stream, x["q"].device, (*x.values(), dO, saved, dfinal, workspace),
+                          lambda: delta_backward(cfg, x, dO, saved, dfinal, workspace))
     dev, st = _delta_inputs(cfg, x)
     S0, start = _delta_rest(cfg, x, dev)
     _check(dO, "dO", cfg.shape("v"), cfg.io, dev)
@@ -524,7 +546,7 @@ def delta_backward(cfg: DeltaConfig, x: Dict[str, torch.Tensor], dO: torch.Tenso
         workspace = _bytes(cfg.size(TNT_WS_BWD if saved is not None else TNT_WS_BWD_RECOMPUTE), dev)
     s = tnt_delta_bwd(cfg, tnt_delta_strides(*st), x["q"], x["k"], x["v"], x["g"], x["lr"], start,
                       S0, dO, dfinal, saved, out["dq"], out["dk"], out["dv"], out["dg"], out["dlr"],
-                      dS0, workspace, stream=_stream_of(dev, stream))
+                      dS0, workspace, stream=_current(dev))
     if s != 0:
         raise TntError(s, "tnt_delta_bwd")
     if dS0 is not None:
@@ -536,6 +558,9 @@ def delta_step(cfg: DeltaConfig, x: Dict[str, torch.Tensor], state: torch.Tensor
                slots: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Run tnt_delta_step over the cfg.L tokens of ``x``: ``state`` [slots][H][dk][dv] is updated
     in place, ``slots`` [B] (int32) names each sequence's state (outside: padding).  Returns o."""
+    if stream is not None and x["q"].is_cuda:
+        return _on_stream(stream, x["q"].device, (*x.values(), state, slots),
+                          lambda: delta_step(cfg, x, state, slots))
     dev, st = _delta_inputs(cfg, x)
     _check(state, "state", (state.shape[0], cfg.H, cfg.dk, cfg.dv), torch.float32, dev, True)
     if slots is not None:
@@ -543,7 +568,7 @@ def delta_step(cfg: DeltaConfig, x: Dict[str, torch.Tensor], state: torch.Tensor
     o = torch.empty_like(x["v"])
     st[9:12] = o.stride()[:3]
     s = tnt_delta_step(cfg, _delta_strides6(*st), x["q"], x["k"], x["v"], x["g"], x["lr"], state,
-                       state.shape[0], slots, o, stream=_stream_of(dev, stream))
+                       state.shape[0], slots, o, stream=_current(dev))
     if s != 0:
         raise TntError(s, "tnt_delta_step")
     return o
@@ -597,6 +622,9 @@ def orthogonalise(cfg: OrthConfig, G: torch.Tensor, out: Optional[torch.Tensor] 
                   workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Run tnt_orth_update on G [n][rows][cols] (rows or columns of adjacent elements, any other
     strides but those of broadcasts); returns ``out``, by default a new tensor laid out as G."""
+    if stream is not None and G.is_cuda:
+        return _on_stream(stream, G.device, (G, out, workspace),
+                          lambda: orthogonalise(cfg, G, out, workspace))
     _check(G, "G", (cfg.n, cfg.rows, cfg.cols), cfg.io, G.device)
     if out is None:
         out = torch.empty_like(G)
@@ -618,7 +646,7 @@ def orthogonalise(cfg: OrthConfig, G: torch.Tensor, out: Optional[torch.Tensor] 
                             G.stride(0), row(G), out.stride(0), row(out))
     if workspace is None:
         workspace = _bytes(cfg.size, G.device)
-    s = tnt_orth_update(c, cfg.coef, G, out, workspace, stream=_stream_of(G.device, stream))
+    s = tnt_orth_update(c, cfg.coef, G, out, workspace, stream=_current(G.device))
     if s != 0:
         raise TntError(s, "tnt_orth_update")
     return out

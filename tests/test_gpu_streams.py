@@ -1,0 +1,59 @@
+"""The ``stream`` argument of the linear memory's and the update's calls: their buffers belong to that
+stream, and the results equal the calls' on the current stream, bit for bit, whatever the current
+stream is given meanwhile."""
+import pytest
+import torch
+
+from paper_2511_07343_amd import tnt
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def calls():
+    gen = torch.Generator().manual_seed(0)
+    r = lambda *s: torch.randn(*s, generator=gen)
+    unit = lambda t: t / t.norm(dim=-1, keepdim=True)
+    B, H, L, d = 2, 2, 150, 64
+    x = dict(q=unit(r(B, H, L, d)).bfloat16(), k=unit(r(B, H, L, d)).bfloat16(), v=r(B, H, L, d).bfloat16(),
+             g=-r(B, H, L).abs(), lr=torch.sigmoid(r(B, H, L)), S0=r(B, H, d, d))
+    x = {n: t.to(DEV) for n, t in x.items()}
+    dO, G, pool = r(B, H, L, d).bfloat16().to(DEV), r(3, 200, 260).to(DEV), r(B, H, d, d).to(DEV)
+    cfg = tnt.DeltaConfig(B=B, H=H, L=L, dk=d, dv=d)
+    orth = tnt.OrthConfig(n=3, rows=200, cols=260)
+    saved = tnt.delta_forward(cfg, x)[1]
+    torch.cuda.synchronize()
+
+    def step(stream):
+        state = pool.clone()
+        if stream is not None:  # the state's copy is made on the current stream
+            torch.cuda.synchronize()
+        return tnt.delta_step(cfg, x, state, stream=stream), state
+
+    return dict(
+        forward=lambda s: tnt.delta_forward(cfg, x, final_state=True, stream=s)[::2],
+        backward=lambda s: tuple(tnt.delta_backward(cfg, x, dO, saved=saved, stream=s).values()),
+        recompute=lambda s: tuple(tnt.delta_backward(cfg, x, dO, stream=s).values()),
+        step=step,
+        update=lambda s: (tnt.orthogonalise(orth, G, stream=s),))
+
+
+@pytest.mark.parametrize("name", ["forward", "backward", "recompute", "step", "update"])
+@pytest.mark.parametrize("raw", [False, True])
+def test_a_given_stream(name, raw, monkeypatch):
+    call = calls()[name]
+    want = [t.clone() for t in call(None)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    made = []
+    empty = tnt._bytes
+    monkeypatch.setattr(tnt, "_bytes", lambda n, dev: made.append(torch.cuda.current_stream().cuda_stream) or empty(n, dev))
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(2_000_000)  # the call's kernels wait behind this
+    got = call(side.cuda_stream if raw else side)
+    # memory that the call has dropped must not come back to the current stream yet
+    held = [torch.full((1 << 16,), float("nan"), device=DEV) for _ in range(200)]
+    torch.cuda.synchronize()
+    assert all(s == side.cuda_stream for s in made) and (made or name == "step")
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.cuda.current_stream() == torch.cuda.default_stream() and len(held) == 200
