@@ -464,9 +464,18 @@ def _delta_inputs(cfg: DeltaConfig, x):
     return dev, st
 
 
+def _place(dev, **buffers):
+    """The tensors are on a GPU, and the caller's buffers there too."""
+    if dev.type != "cuda":
+        raise ValueError(f"expected tensors on a GPU, got {dev}")
+    for name, t in buffers.items():
+        if t is not None and (t.device != dev or not t.is_contiguous()):
+            raise ValueError(f"{name}: expected a contiguous tensor on {dev}")
+
+
 def _current(dev):
     """The current stream of the tensors' device."""
-    return torch._C._cuda_getCurrentRawStream(dev.index) if dev.type == "cuda" else None
+    return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
 def _on_stream(stream, dev, inputs, call):
@@ -508,6 +517,7 @@ def delta_forward(cfg: DeltaConfig, x: Dict[str, torch.Tensor], save: bool = Tru
                           lambda: delta_forward(cfg, x, save, final_state, workspace))
     dev, st = _delta_inputs(cfg, x)
     S0, start = _delta_rest(cfg, x, dev)
+    _place(dev, workspace=workspace)
     o = torch.empty_like(x["v"])
     st[9:12] = o.stride()[:3]
     fin = (torch.empty(cfg.sequences, cfg.H, cfg.dk, cfg.dv, dtype=torch.float32, device=dev)
@@ -537,6 +547,7 @@ def delta_backward(cfg: DeltaConfig, x: Dict[str, torch.Tensor], dO: torch.Tenso
         _check(dfinal, "dfinal", (cfg.sequences, cfg.H, cfg.dk, cfg.dv), torch.float32, dev, True)
     if dO.stride(3) != 1 and cfg.dv > 1 and dO.numel():
         raise ValueError("dO: elements of a token must be adjacent")
+    _place(dev, workspace=workspace, saved=saved)
     st += dO.stride()[:3]
     out = {"d" + n: torch.empty_like(x[n]) for n in _DELTA_IN}
     for t in out.values():
@@ -565,6 +576,7 @@ def delta_step(cfg: DeltaConfig, x: Dict[str, torch.Tensor], state: torch.Tensor
     _check(state, "state", (state.shape[0], cfg.H, cfg.dk, cfg.dv), torch.float32, dev, True)
     if slots is not None:
         _check(slots, "slots", (cfg.B,), torch.int32, dev, True)
+    _place(dev)
     o = torch.empty_like(x["v"])
     st[9:12] = o.stride()[:3]
     s = tnt_delta_step(cfg, _delta_strides6(*st), x["q"], x["k"], x["v"], x["g"], x["lr"], state,
@@ -644,6 +656,7 @@ def orthogonalise(cfg: OrthConfig, G: torch.Tensor, out: Optional[torch.Tensor] 
         row = lambda t: t.stride(r) if t.shape[r] > 1 else side
         c = tnt_orth_config(base.n, base.rows, base.cols, base.steps, base.dtype, base.eps, base.scale,
                             G.stride(0), row(G), out.stride(0), row(out))
+    _place(G.device, workspace=workspace)
     if workspace is None:
         workspace = _bytes(cfg.size, G.device)
     s = tnt_orth_update(c, cfg.coef, G, out, workspace, stream=_current(G.device))

@@ -138,3 +138,26 @@ def test_oracle_without_decay_solves_recall():
 def test_strides_layout_matches_header():
     assert ctypes.sizeof(tnt.tnt_delta_strides) == 12 * 3 * 8
     assert ctypes.sizeof(tnt.tnt_delta_config) == 36
+
+
+def test_host_tensors_are_refused(monkeypatch):
+    """Tensors in host memory never reach the library, given workspaces and saved buffers among them."""
+    c = cfg(B=1, H=2, Hk=1, L=3, dk=8, dv=8)
+    x = {n: torch.zeros(c.shape(n), dtype=c.io if n in "qkv" else torch.float32)
+         for n in ("q", "k", "v", "g", "lr")}
+    dO, state = torch.zeros(c.shape("v"), dtype=c.io), torch.zeros(4, 2, 8, 8)
+    size = lambda kind: torch.empty(c.size(kind), dtype=torch.uint8)
+
+    def reached(*a, **kw):
+        raise AssertionError("the library was called")
+
+    for n in ("tnt_delta_fwd", "tnt_delta_bwd", "tnt_delta_step"):
+        monkeypatch.setattr(tnt, n, reached)
+    for call in (lambda s: tnt.delta_forward(c, x, stream=s),
+                 lambda s: tnt.delta_forward(c, x, workspace=size(tnt.TNT_WS_FWD), stream=s),
+                 lambda s: tnt.delta_backward(c, x, dO, stream=s),
+                 lambda s: tnt.delta_backward(c, x, dO, saved=size("saved"), workspace=size(tnt.TNT_WS_BWD), stream=s),
+                 lambda s: tnt.delta_step(c, x, state, stream=s)):
+        for stream in (None, 0):
+            with pytest.raises(ValueError, match="GPU"):
+                call(stream)

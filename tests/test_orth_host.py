@@ -92,3 +92,17 @@ def test_broadcast_extents_are_refused(shape, stride0):
         tnt.orthogonalise(cfg, wide)
     with pytest.raises(ValueError, match="out: broadcast"):
         tnt.orthogonalise(cfg, whole, out=wide)
+
+
+def test_host_tensors_are_refused(monkeypatch):
+    """Matrices in host memory never reach the library."""
+    def reached(*a, **kw):
+        raise AssertionError("the library was called")
+
+    monkeypatch.setattr(tnt, "tnt_orth_update", reached)
+    cfg = tnt.OrthConfig(n=2, rows=4, cols=6)
+    for stream in (None, 0):
+        with pytest.raises(ValueError, match="GPU"):
+            tnt.orthogonalise(cfg, torch.zeros(2, 4, 6), stream=stream)
+        with pytest.raises(ValueError, match="GPU"):
+            tnt.orthogonalise(cfg, torch.zeros(2, 4, 6), workspace=torch.empty(16, dtype=torch.uint8), stream=stream)
