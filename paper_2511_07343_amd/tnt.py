@@ -464,13 +464,10 @@ def _delta_inputs(cfg: DeltaConfig, x):
     return dev, st
 
 
-def _place(dev, **buffers):
-    """The tensors are on a GPU, and the caller's buffers there too."""
-    if dev.type != "cuda":
-        raise ValueError(f"expected tensors on a GPU, got {dev}")
-    for name, t in buffers.items():
-        if t is not None and (t.device != dev or not t.is_contiguous()):
-            raise ValueError(f"{name}: expected a contiguous tensor on {dev}")
+def _place(dev, name, t):
+    """A caller's buffer is where the tensors are."""
+    if t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor on {dev}")
 
 
 def _current(dev):
@@ -478,13 +475,23 @@ def _current(dev):
     return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
+def _elsewhere(stream, dev) -> bool:
+    """A call that is not for the current stream of the current device; refused off the GPUs."""
+    if dev.index is None:
+        raise ValueError(f"expected tensors on a GPU, got {dev}")
+    return stream is not None or dev.index != torch._C._cuda_getDevice()
+
+
 def _on_stream(stream, dev, inputs, call):
-    """``call()`` with ``stream`` (torch's, or a handle) as the current one: what it allocates is
+    """``call()`` with ``stream`` (torch's, or a handle; None: the device's current one) as the
+    current one, and the tensors' device the current device: what it allocates is
     that stream's, so that a buffer dropped on return is given to nothing that does not wait for the
     kernels using it.  The inputs are marked as used there, the outputs as used on the caller's
     stream.  Ordering the two streams is the caller's, as with any torch work on a side stream."""
     back = torch.cuda.current_stream(dev)
-    if not hasattr(stream, "cuda_stream"):
+    if stream is None:
+        stream = back
+    elif not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(stream, device=dev)
     with torch.cuda.stream(stream):
         out = call()
@@ -512,12 +519,13 @@ def delta_forward(cfg: DeltaConfig, x: Dict[str, torch.Tensor], save: bool = Tru
                   stream=None):
     """Run tnt_delta_fwd on ``x`` (q, k, v, g, lr and, where given, S0 and seq_start; any strides
     with adjacent elements); returns (o in v's layout, saved or None, final state or None)."""
-    if stream is not None and x["q"].is_cuda:
-        return _on_stream(stream, x["q"].device, (*x.values(), workspace),
-                          lambda: delta_forward(cfg, x, save, final_state, workspace))
     dev, st = _delta_inputs(cfg, x)
     S0, start = _delta_rest(cfg, x, dev)
-    _place(dev, workspace=workspace)
+    if workspace is not None:
+        _place(dev, "workspace", workspace)
+    if _elsewhere(stream, dev):
+        return _on_stream(stream, dev, (*x.values(), workspace),
+                          lambda: delta_forward(cfg, x, save, final_state, workspace))
     o = torch.empty_like(x["v"])
     st[9:12] = o.stride()[:3]
     fin = (torch.empty(cfg.sequences, cfg.H, cfg.dk, cfg.dv, dtype=torch.float32, device=dev)
@@ -537,9 +545,6 @@ def delta_backward(cfg: DeltaConfig, x: Dict[str, torch.Tensor], dO: torch.Tenso
                    workspace: Optional[torch.Tensor] = None, stream=None):
     """Run tnt_delta_bwd; returns the gradients of sum(dO * o) + sum(dfinal * final state) in
     their inputs' layouts (dS0 where there is an S0).  ``saved`` None: recomputed."""
-    if stream is not None and x["q"].is_cuda:
-        return _on_stream(stream, x["q"].device, (*x.values(), dO, saved, dfinal, workspace),
-                          lambda: delta_backward(cfg, x, dO, saved, dfinal, workspace))
     dev, st = _delta_inputs(cfg, x)
     S0, start = _delta_rest(cfg, x, dev)
     _check(dO, "dO", cfg.shape("v"), cfg.io, dev)
@@ -547,7 +552,12 @@ def delta_backward(cfg: DeltaConfig, x: Dict[str, torch.Tensor], dO: torch.Tenso
         _check(dfinal, "dfinal", (cfg.sequences, cfg.H, cfg.dk, cfg.dv), torch.float32, dev, True)
     if dO.stride(3) != 1 and cfg.dv > 1 and dO.numel():
         raise ValueError("dO: elements of a token must be adjacent")
-    _place(dev, workspace=workspace, saved=saved)
+    for n, t in (("workspace", workspace), ("saved", saved)):
+        if t is not None:
+            _place(dev, n, t)
+    if _elsewhere(stream, dev):
+        return _on_stream(stream, dev, (*x.values(), dO, saved, dfinal, workspace),
+                          lambda: delta_backward(cfg, x, dO, saved, dfinal, workspace))
     st += dO.stride()[:3]
     out = {"d" + n: torch.empty_like(x[n]) for n in _DELTA_IN}
     for t in out.values():
@@ -569,14 +579,13 @@ def delta_step(cfg: DeltaConfig, x: Dict[str, torch.Tensor], state: torch.Tensor
                slots: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Run tnt_delta_step over the cfg.L tokens of ``x``: ``state`` [slots][H][dk][dv] is updated
     in place, ``slots`` [B] (int32) names each sequence's state (outside: padding).  Returns o."""
-    if stream is not None and x["q"].is_cuda:
-        return _on_stream(stream, x["q"].device, (*x.values(), state, slots),
-                          lambda: delta_step(cfg, x, state, slots))
     dev, st = _delta_inputs(cfg, x)
     _check(state, "state", (state.shape[0], cfg.H, cfg.dk, cfg.dv), torch.float32, dev, True)
     if slots is not None:
         _check(slots, "slots", (cfg.B,), torch.int32, dev, True)
-    _place(dev)
+    if _elsewhere(stream, dev):
+        return _on_stream(stream, dev, (*x.values(), state, slots),
+                          lambda: delta_step(cfg, x, state, slots))
     o = torch.empty_like(x["v"])
     st[9:12] = o.stride()[:3]
     s = tnt_delta_step(cfg, _delta_strides6(*st), x["q"], x["k"], x["v"], x["g"], x["lr"], state,
@@ -634,10 +643,8 @@ def orthogonalise(cfg: OrthConfig, G: torch.Tensor, out: Optional[torch.Tensor] 
                   workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Run tnt_orth_update on G [n][rows][cols] (rows or columns of adjacent elements, any other
     strides but those of broadcasts); returns ``out``, by default a new tensor laid out as G."""
-    if stream is not None and G.is_cuda:
-        return _on_stream(stream, G.device, (G, out, workspace),
-                          lambda: orthogonalise(cfg, G, out, workspace))
     _check(G, "G", (cfg.n, cfg.rows, cfg.cols), cfg.io, G.device)
+    given = out
     if out is None:
         out = torch.empty_like(G)
     else:
@@ -656,7 +663,11 @@ def orthogonalise(cfg: OrthConfig, G: torch.Tensor, out: Optional[torch.Tensor] 
         row = lambda t: t.stride(r) if t.shape[r] > 1 else side
         c = tnt_orth_config(base.n, base.rows, base.cols, base.steps, base.dtype, base.eps, base.scale,
                             G.stride(0), row(G), out.stride(0), row(out))
-    _place(G.device, workspace=workspace)
+    if workspace is not None:
+        _place(G.device, "workspace", workspace)
+    if _elsewhere(stream, G.device):
+        return _on_stream(stream, G.device, (G, given, workspace),
+                          lambda: orthogonalise(cfg, G, given, workspace))
     if workspace is None:
         workspace = _bytes(cfg.size, G.device)
     s = tnt_orth_update(c, cfg.coef, G, out, workspace, stream=_current(G.device))

@@ -57,3 +57,31 @@ def test_a_given_stream(name, raw, monkeypatch):
     assert all(s == side.cuda_stream for s in made) and (made or name == "step")
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert torch.cuda.current_stream() == torch.cuda.default_stream() and len(held) == 200
+
+
+@pytest.mark.parametrize("name", ["forward", "backward", "step", "update"])
+def test_another_current_device(name, monkeypatch):
+    """Tensors of a device that is not the current one: the library's launches go to the current device,
+    so the tensors' is made current first."""
+    call = calls()[name]
+    want = [t.clone() for t in call(None)]
+    seen, entered, real = [], [], torch.cuda.stream
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0 if entered else 1)
+
+    class entering:
+        def __init__(self, s):
+            self.s, self.inner = s, real(s)
+
+        def __enter__(self):
+            entered.append(self.s)
+            seen.append(self.s.device)
+            return self.inner.__enter__()
+
+        def __exit__(self, *e):
+            entered.pop()
+            return self.inner.__exit__(*e)
+
+    monkeypatch.setattr(torch.cuda, "stream", entering)
+    got = call(None)
+    torch.cuda.synchronize(DEV)
+    assert seen == [torch.device(DEV)] and all(torch.equal(a, b) for a, b in zip(got, want))
