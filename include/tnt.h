@@ -381,7 +381,7 @@ typedef struct {
   int64_t out_batch, out_row; /* element strides of out, 0: contiguous           */
 } tnt_orth_config;
 
-/* Bytes of device workspace (0: invalid configuration). */
+/* Bytes of device workspace, of a configuration with its strides (0: invalid). */
 size_t tnt_orth_workspace_size(const tnt_orth_config* cfg);
 
 tnt_status tnt_orth_update(const tnt_orth_config* cfg, const float* coef, const void* G,

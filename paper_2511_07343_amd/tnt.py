@@ -624,6 +624,7 @@ class OrthConfig:
 
     @property
     def size(self) -> int:
+        """Bytes of workspace for contiguous tensors (others: ``tnt_orth_workspace_size``)."""
         if self._size is None:
             self._size = lib().tnt_orth_workspace_size(self.ref)
         return self._size
@@ -669,7 +670,8 @@ def orthogonalise(cfg: OrthConfig, G: torch.Tensor, out: Optional[torch.Tensor] 
         return _on_stream(stream, G.device, (G, given, workspace),
                           lambda: orthogonalise(cfg, G, given, workspace))
     if workspace is None:
-        workspace = _bytes(cfg.size, G.device)
+        size = cfg.size if c is cfg.c else lib().tnt_orth_workspace_size(ctypes.byref(c))
+        workspace = _bytes(size, G.device)
     s = tnt_orth_update(c, cfg.coef, G, out, workspace, stream=_current(G.device))
     if s != 0:
         raise TntError(s, "tnt_orth_update")

@@ -178,3 +178,14 @@ def test_bf16_is_the_result_rounded_once(n, r, c):
         want = O.orthogonalise(G[i], [MUON] * 5).to(torch.bfloat16).double()
         e = ((out[i] - want).norm() / want.norm()).item()
         assert check_err(f"orth rounded {n}x{r}x{c}", f"out[{i}]", e, (1e-4 * 2.0 ** -7) ** 0.5), (i, e)
+
+
+def test_rows_far_apart():
+    """Rows 2^21 elements apart, past the 32-bit offsets of the form for one workgroup."""
+    G = matrices(1, 8, 12, torch.float32, seed=9)
+    far = torch.empty_strided((1, 8, 12), (1 << 24, 1 << 21, 1), device=DEV)
+    far.copy_(G)
+    out = torch.empty(1, 8, 12, device=DEV)
+    tnt.orthogonalise(tnt.OrthConfig(n=1, rows=8, cols=12), far, out=out)
+    torch.cuda.synchronize()
+    check("orth far rows", out, G, [MUON] * 5)

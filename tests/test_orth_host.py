@@ -106,3 +106,29 @@ def test_host_tensors_are_refused(monkeypatch):
             tnt.orthogonalise(cfg, torch.zeros(2, 4, 6), stream=stream)
         with pytest.raises(ValueError, match="GPU"):
             tnt.orthogonalise(cfg, torch.zeros(2, 4, 6), workspace=torch.empty(16, dtype=torch.uint8), stream=stream)
+
+
+def _handed_over(monkeypatch, cfg, *args, **kw):
+    """The structure and the workspace size that a call on host tensors would hand to the library."""
+    seen = {}
+
+    def update(c, coef, G, out, workspace, ws_bytes=None, stream=None):
+        seen.update(c=c, ws=workspace.numel())
+        return 0
+
+    monkeypatch.setattr(tnt, "tnt_orth_update", update)
+    monkeypatch.setattr(tnt, "_elsewhere", lambda stream, dev: False)
+    monkeypatch.setattr(tnt, "_current", lambda dev: 0)
+    tnt.orthogonalise(cfg, *args, **kw)
+    return seen
+
+
+@pytest.mark.parametrize("flip", [False, True])
+def test_workspace_of_rows_far_apart(flip, monkeypatch):
+    """Rows 2^21 elements apart leave the form that needs no workspace: the binding asks for what the
+    strides need."""
+    G = torch.empty_strided((1, 8, 8), (1 << 24, 1, 1 << 21) if flip else (1 << 24, 1 << 21, 1))
+    seen = _handed_over(monkeypatch, tnt.OrthConfig(n=1, rows=8, cols=8), G, out=torch.empty_strided(
+        (1, 8, 8), (64, 1, 8) if flip else (64, 8, 1)))
+    need = tnt.lib().tnt_orth_workspace_size(ctypes.byref(seen["c"]))
+    assert need > 16 and seen["ws"] == need
