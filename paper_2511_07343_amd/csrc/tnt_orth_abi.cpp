@@ -24,10 +24,13 @@ tnt_status validate(const tnt_orth_config* c) {
   if (c->steps > ORTH_MAX_STEPS || c->rows > MAX_SIDE || c->cols > MAX_SIDE) return TNT_ERR_UNSUPPORTED;
   if (!(c->eps >= 0.f) || !std::isfinite(c->eps) || !std::isfinite(c->scale)) return TNT_ERR_ARG;
   if (c->g_row < 0 || c->g_batch < 0 || c->out_row < 0 || c->out_batch < 0) return TNT_ERR_ARG;
-  // outputs of rows or matrices that overlap
+  // outputs that overlap: rows within a matrix, and matrices neither one after the other nor
+  // with their rows side by side
   if (c->out_row && c->out_row < c->cols) return TNT_ERR_ARG;
   const int64_t orow = c->out_row ? c->out_row : c->cols;
-  if (c->out_batch && c->n > 1 && c->out_batch < (int64_t)(c->rows - 1) * orow + c->cols) return TNT_ERR_ARG;
+  if (c->out_batch && c->n > 1 && c->out_batch < (int64_t)(c->rows - 1) * orow + c->cols &&
+      (c->out_batch < c->cols || orow < (int64_t)(c->n - 1) * c->out_batch + c->cols))
+    return TNT_ERR_ARG;
   return TNT_OK;
 }
 

@@ -189,3 +189,17 @@ def test_rows_far_apart():
     tnt.orthogonalise(tnt.OrthConfig(n=1, rows=8, cols=12), far, out=out)
     torch.cuda.synchronize()
     check("orth far rows", out, G, [MUON] * 5)
+
+
+@pytest.mark.parametrize("r,c", [(40, 60), (150, 140)])
+def test_transposed_batch(r, c):
+    """[rows][matrices][cols] memory: the same results in the same layout, in place too."""
+    G = matrices(3, r, c, torch.float32, seed=10)
+    want = run(G.to(DEV))
+    side = G.to(DEV).transpose(0, 1).contiguous().transpose(0, 1)
+    cfg = tnt.OrthConfig(n=3, rows=r, cols=c)
+    out = tnt.orthogonalise(cfg, side)
+    assert out.stride() == side.stride() and torch.equal(out, want)
+    tnt.orthogonalise(cfg, side, out=side)
+    torch.cuda.synchronize()
+    assert torch.equal(side, want)

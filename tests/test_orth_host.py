@@ -132,3 +132,21 @@ def test_workspace_of_rows_far_apart(flip, monkeypatch):
         (1, 8, 8), (64, 1, 8) if flip else (64, 8, 1)))
     need = tnt.lib().tnt_orth_workspace_size(ctypes.byref(seen["c"]))
     assert need > 16 and seen["ws"] == need
+
+
+@pytest.mark.parametrize("strides,code", [
+    (dict(out_row=600, out_batch=300), None), (dict(out_row=603, out_batch=301), None),  # rows of the batch in turn
+    (dict(out_row=300, out_batch=60000), None),
+    (dict(out_row=599, out_batch=300), 7), (dict(out_row=600, out_batch=299), 7), (dict(out_row=600, out_batch=301), 7),
+    (dict(out_row=300, out_batch=59999), 7)])
+def test_outputs_that_do_not_overlap(strides, code):
+    """Matrices one after the other, or rows of all matrices side by side (2 matrices of 200 x 300)."""
+    assert call(ptr=0, **strides) == (code or 1)  # without pointers the call ends at them
+
+
+def test_transposed_batch_keeps_its_layout(monkeypatch):
+    """Per-head matrices as [rows][heads][cols]: the default output has the same layout."""
+    G = torch.zeros(8, 3, 6).transpose(0, 1)
+    seen = _handed_over(monkeypatch, tnt.OrthConfig(n=3, rows=8, cols=6), G)
+    assert (seen["c"].out_batch, seen["c"].out_row) == (6, 18)
+    assert tnt.lib().tnt_orth_workspace_size(ctypes.byref(seen["c"])) > 0
