@@ -115,7 +115,7 @@ def serve(layer, x, prompt):
     """The layer on x [B][L][D]: a prompt through the chunked forward, then token by token."""
     B, L, _ = x.shape
     z = {n: t.detach() for n, t in layer.inputs(x).items()}
-    cut = lambda a, b: {n: t[:, :, a:b].clone() for n, t in z.items()}
+    cut = lambda a, b: {n: t[:, :, a:b] for n, t in z.items()}
     o, _, fin = tnt.delta_forward(config(B, prompt), cut(0, prompt), save=False, final_state=True)
     slots = torch.arange(B, device=DEV, dtype=torch.int32).flip(0) + 1  # anywhere in a pool
     pool = torch.zeros(B + 2, H, DK, DV, device=DEV)

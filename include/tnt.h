@@ -297,7 +297,8 @@ tnt_status tnt_dbg_chunk_grads(const tnt_config* cfg, int32_t b, int32_t h, int3
  *    adjacent), e.g. of views of [B][L][heads][d] projections; NULL: the
  *    contiguous layouts above.  Strides of q, k, v, o and their gradients are
  *    multiples of 16 bytes (TNT_ERR_ALIGN), tokens at most 2^24 elements apart
- *    (TNT_ERR_UNSUPPORTED).  Inputs may be broadcast (stride 0);
+ *    (TNT_ERR_UNSUPPORTED); g, lr, dg, dlr, seq_start and slots may begin at any
+ *    element, every other pointer is 16-byte aligned.  Inputs may be broadcast (stride 0);
  *    outputs may not (TNT_ERR_ARG).  The gradient of a broadcast input is written
  *    per element: the caller sums it.
  *  - n_seq > 0 packs sequences of different lengths into one row (B == 1):

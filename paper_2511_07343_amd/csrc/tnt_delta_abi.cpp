@@ -73,6 +73,8 @@ bool plan_of(const tnt_delta_config* c, Plan* p) {
 }
 
 bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
+// read and written an element of four bytes at a time
+bool split_element(const void* p) { return ((uintptr_t)p & 3u) != 0; }
 
 // element strides of [B][heads][L][d] or, d = 0, of the gates [B][heads][L]
 Str contiguous(int heads, int L, int d) {
@@ -202,10 +204,11 @@ tnt_status tnt_delta_fwd(const tnt_delta_config* cfg, const tnt_delta_strides* s
   if (s != TNT_OK) return s;
   if ((cfg->L && (!q || !k || !v || !g || !lr || !o)) || !workspace || (cfg->n_seq && !seq_start))
     return TNT_ERR_NULL;
-  for (const void* p : {q, k, v, (const void*)g, (const void*)lr, (const void*)seq_start, (const void*)S0,
-                        (const void*)o, (const void*)final_state, (const void*)saved,
-                        (const void*)workspace})
+  for (const void* p : {q, k, v, (const void*)S0, (const void*)o, (const void*)final_state,
+                        (const void*)saved, (const void*)workspace})
     if (p && misaligned(p)) return TNT_ERR_ALIGN;
+  for (const void* p : {(const void*)g, (const void*)lr, (const void*)seq_start})
+    if (p && split_element(p)) return TNT_ERR_ALIGN;
   if (ws_bytes < (saved ? c.p.fwd - up256(c.p.saved) : c.p.fwd)) return TNT_ERR_WORKSPACE;
   if (saved && saved_bytes < c.p.saved) return TNT_ERR_WORKSPACE;
   DeltaArgs& a = c.a;
@@ -232,10 +235,11 @@ tnt_status tnt_delta_bwd(const tnt_delta_config* cfg, const tnt_delta_strides* s
   if ((cfg->L && (!q || !k || !v || !g || !lr || !dO || !dq || !dk || !dv || !dg || !dlr)) ||
       !workspace || (cfg->n_seq && !seq_start))
     return TNT_ERR_NULL;
-  for (const void* p : {q, k, v, (const void*)g, (const void*)lr, (const void*)seq_start, (const void*)S0,
-                        dO, (const void*)dfinal, saved, (const void*)dq, (const void*)dk, (const void*)dv,
-                        (const void*)dg, (const void*)dlr, (const void*)dS0, (const void*)workspace})
+  for (const void* p : {q, k, v, (const void*)S0, dO, (const void*)dfinal, saved, (const void*)dq,
+                        (const void*)dk, (const void*)dv, (const void*)dS0, (const void*)workspace})
     if (p && misaligned(p)) return TNT_ERR_ALIGN;
+  for (const void* p : {(const void*)g, (const void*)lr, (const void*)seq_start, (const void*)dg, (const void*)dlr})
+    if (p && split_element(p)) return TNT_ERR_ALIGN;
   if (ws_bytes < (saved ? c.p.bwd : c.p.bwd_re)) return TNT_ERR_WORKSPACE;
   if (saved && saved_bytes < c.p.saved) return TNT_ERR_WORKSPACE;
   DeltaArgs& a = c.a;
@@ -266,9 +270,10 @@ tnt_status tnt_delta_step(const tnt_delta_config* cfg, const tnt_delta_strides* 
   if (cfg->n_seq || n_slots <= 0 || (!slots && n_slots < cfg->B)) return TNT_ERR_SHAPE;
   if (cfg->L == 0) return TNT_OK;
   if (!q || !k || !v || !g || !lr || !state || !o) return TNT_ERR_NULL;
-  for (const void* p : {q, k, v, (const void*)g, (const void*)lr, (const void*)state, (const void*)slots,
-                        (const void*)o})
+  for (const void* p : {q, k, v, (const void*)state, (const void*)o})
     if (p && misaligned(p)) return TNT_ERR_ALIGN;
+  for (const void* p : {(const void*)g, (const void*)lr, (const void*)slots})
+    if (p && split_element(p)) return TNT_ERR_ALIGN;
   if ((int64_t)cfg->B * cfg->H * 8 > INT32_MAX / 8) return TNT_ERR_UNSUPPORTED;
   DeltaStepArgs a{};
   a.q = q; a.k = k; a.v = v; a.g = g; a.lr = lr; a.state = state; a.slot = slots; a.o = o;

@@ -161,3 +161,29 @@ def test_host_tensors_are_refused(monkeypatch):
         for stream in (None, 0):
             with pytest.raises(ValueError, match="GPU"):
                 call(stream)
+
+
+@pytest.mark.parametrize("n", ["g", "lr", "dg", "dlr", "seq_start", "slots"])
+@pytest.mark.parametrize("off,ok", [(4, True), (8, True), (2, False)])
+def test_element_wise_tensors_at_any_element(n, off, ok):
+    """Gates, their gradients, offsets and slots are read and written one element at a time: they may
+    begin anywhere, as slices of longer tensors do.  (The calls end at their workspace or at a
+    broadcast output.)"""
+    at = lambda name: P + off if name == n else P
+    seq = cfg(B=1, n_seq=2) if n == "seq_start" else cfg()
+    start = at("seq_start") if seq.n_seq else None
+    want = 4 if ok else 5
+    if n in ("g", "lr", "seq_start"):
+        assert tnt.tnt_delta_fwd(seq, None, P, P, P, at("g"), at("lr"), start, None, P, None, None, P,
+                                 ws_bytes=0, stream=0) == want
+    if n != "slots":
+        assert tnt.tnt_delta_bwd(seq, None, P, P, P, at("g"), at("lr"), start, None, P, None, None, P, P, P,
+                                 at("dg"), at("dlr"), None, P, ws_bytes=0, stream=0) == want
+    if n in ("g", "lr", "slots"):
+        c, s = cfg(), []
+        for name in ("q", "k", "v", "v", "g", "g"):
+            s += torch.empty(c.shape(name), device="meta").stride()[:3]
+        s[9] = 0
+        got = tnt.tnt_delta_step(c, tnt.tnt_delta_strides(*s), P, P, P, at("g"), at("lr"), P, 8, at("slots"), P,
+                                 stream=0)
+        assert got == (7 if ok else 5)

@@ -400,3 +400,29 @@ def test_step_slot_out_of_range_is_padding():
     o = tnt.delta_step(cfg, gpu(x), state, slots=torch.tensor([3, 1 << 30], dtype=torch.int32, device=DEV))
     torch.cuda.synchronize()
     assert torch.equal(o, torch.zeros_like(o)) and torch.equal(state, torch.ones_like(state))
+
+
+def test_slices_of_a_sequence():
+    """Tokens cut out of a longer sequence, gates that begin at any element, slots and offsets inside
+    longer lists: the same bits as from copies."""
+    B, H, L, d = 2, 2, 100, 64
+    x = gpu(make(B, H, L, d, d, seed=41))
+    pool = torch.randn(5, H, d, d, generator=torch.Generator().manual_seed(2)).to(DEV)
+    one = tnt.DeltaConfig(B=B, H=H, L=1, dk=d, dv=d)
+    slots = torch.tensor([9, 4, 1], dtype=torch.int32, device=DEV)[1:]
+    for t in range(4):
+        cut = {n: z[:, :, t:t + 1] for n, z in x.items()}
+        a, b = pool.clone(), pool.clone()
+        got = tnt.delta_step(one, cut, a, slots=slots)
+        want = tnt.delta_step(one, {n: z.clone() for n, z in cut.items()}, b, slots=slots.clone())
+        assert torch.equal(got, want) and torch.equal(a, b) and not torch.equal(a, pool)
+    for first in (1, 2, 3):
+        cfg = tnt.DeltaConfig(B=1, H=H, L=L - first, dk=d, dv=d, n_seq=2)
+        cut = {n: z[:1, :, first:] for n, z in x.items()}
+        cut["seq_start"] = torch.tensor([7, 0, 60, L - first], dtype=torch.int32, device=DEV)[1:]
+        whole = {n: z.clone() for n, z in cut.items()}
+        o, saved, _ = tnt.delta_forward(cfg, cut)
+        wo, wsaved, _ = tnt.delta_forward(cfg, whole)
+        g = tnt.delta_backward(cfg, cut, cut["dO"], saved=saved)
+        w = tnt.delta_backward(cfg, whole, whole["dO"], saved=wsaved)
+        assert torch.equal(o, wo) and all(torch.equal(g[n], w[n]) for n in w)
