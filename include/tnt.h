@@ -372,7 +372,8 @@ tnt_status tnt_delta_step(const tnt_delta_config* cfg, const tnt_delta_strides* 
  *  - Everything is computed to fp32 accuracy, whatever the matrices' type and sizes;
  *    outputs are rounded once.
  *  - A zero matrix gives zeros (eps > 0); a NaN or infinite entry spoils its own matrix
- *    alone.  Any sizes from 1 to 32768, any alignment of rows; out may be G. */
+ *    alone.  Any sizes from 1 to 32768; matrices and rows begin at any element; out may
+ *    be G. */
 typedef struct {
   int32_t n, rows, cols;      /* n >= 0 matrices                                 */
   int32_t steps;              /* 1 .. 16                                         */

@@ -281,9 +281,9 @@ __global__ __launch_bounds__(256) void orth_norm_kernel(OrthArgs a) {
   const int b = blockIdx.x / a.parts, s = blockIdx.x - b * a.parts, tid = threadIdx.x;
   const int64_t g0 = (int64_t)b * a.gb;
   double ss = 0.;
-  // rows of whole 16-byte pieces: 4 of them a lane at once
+  // rows of whole 16-byte pieces at 16 bytes: 4 of them a lane at once
   const int64_t el = a.bf16 ? 8 : 4;
-  if (a.cols % el == 0 && a.gr % el == 0 && a.gb % el == 0) {
+  if ((uintptr_t)a.G % 16 == 0 && a.cols % el == 0 && a.gr % el == 0 && a.gb % el == 0) {
     const uint32_t per = a.cols / (int)el, all = a.rows * per, hop = a.parts * 256;  // all <= 2^28
     for (uint32_t i0 = s * 256 + tid; i0 < all; i0 += 4 * hop) {
       f4 v[4];

@@ -87,7 +87,7 @@ Lay lay_of(const tnt_orth_config* c) {
   return l;
 }
 
-bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
+bool misaligned(const void* p, size_t to) { return (uintptr_t)p % to != 0; }
 
 }  // namespace
 
@@ -118,8 +118,8 @@ tnt_status tnt_orth_update(const tnt_orth_config* cfg, const float* coef, const 
   if (!G || !out) return TNT_ERR_NULL;
   const Lay l = lay_of(cfg);
   if (l.bytes && !workspace) return TNT_ERR_NULL;
-  for (const void* p : {G, (const void*)out, (const void*)workspace})
-    if (p && misaligned(p)) return TNT_ERR_ALIGN;
+  const size_t elem = cfg->dtype == TNT_BF16 ? 2 : 4;
+  if (misaligned(G, elem) || misaligned(out, elem) || misaligned(workspace, 16)) return TNT_ERR_ALIGN;
   if (ws_bytes < l.bytes) return TNT_ERR_WORKSPACE;
   if (!l.small && (int64_t)cfg->n * (l.kp / 64) * (l.mp / 64) > INT32_MAX / 256) return TNT_ERR_UNSUPPORTED;
   if (cfg->n > 65535) return TNT_ERR_UNSUPPORTED;

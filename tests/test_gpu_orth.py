@@ -203,3 +203,19 @@ def test_transposed_batch(r, c):
     tnt.orthogonalise(cfg, side, out=side)
     torch.cuda.synchronize()
     assert torch.equal(side, want)
+
+
+@pytest.mark.parametrize("r,c", [(40, 64), (136, 144)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_first_element_anywhere(r, c, dtype):
+    """Matrices that begin inside a buffer, their rows whole 16-byte pieces all the same."""
+    G = matrices(2, r, c, dtype, seed=11)
+    cfg = tnt.OrthConfig(n=2, rows=r, cols=c, dtype=int(dtype == torch.bfloat16))
+    for off in (1, 3):
+        src, dst = (torch.full((2 * r * c + 8,), 7.0, dtype=dtype, device=DEV) for _ in range(2))
+        g, out = (t[off:off + 2 * r * c].view(2, r, c) for t in (src, dst))
+        g.copy_(G)
+        tnt.orthogonalise(cfg, g, out=out)
+        torch.cuda.synchronize()
+        check("orth offset", out, G, [MUON] * 5)
+        assert (dst[:off] == 7).all() and (dst[off + 2 * r * c:] == 7).all()

@@ -150,3 +150,12 @@ def test_transposed_batch_keeps_its_layout(monkeypatch):
     seen = _handed_over(monkeypatch, tnt.OrthConfig(n=3, rows=8, cols=6), G)
     assert (seen["c"].out_batch, seen["c"].out_row) == (6, 18)
     assert tnt.lib().tnt_orth_workspace_size(ctypes.byref(seen["c"])) > 0
+
+
+@pytest.mark.parametrize("dtype,off,ok", [(0, 4, True), (0, 8, True), (0, 2, False), (1, 2, True), (1, 6, True), (1, 1, False)])
+def test_matrices_at_any_element(dtype, off, ok):
+    """G and out begin at any element; the workspace lies at 16 bytes."""
+    cfg = tnt.OrthConfig(n=2, rows=200, cols=300, dtype=dtype)
+    for g, out in ((P + off, P), (P, P + off)):
+        assert tnt.tnt_orth_update(cfg.c, None, g, out, P, ws_bytes=0, stream=0) == (4 if ok else 5)
+    assert tnt.tnt_orth_update(cfg.c, None, P, P, P + 8, ws_bytes=0, stream=0) == 5
