@@ -129,7 +129,7 @@ __global__ __launch_bounds__(512) void orth_small_kernel(OrthArgs a) {
   ss = 0.;
 #pragma unroll
   for (int i = 0; i < 8; ++i) ss += red[i];
-  const float inv = (float)((double)SX / (sqrt(ss) + (double)a.eps));
+  const double inv = (double)SX / (sqrt(ss) + (double)a.eps);  // of a small norm, past fp32
   h8 xh[RP][MT], xl[RP][MT];
 #pragma unroll
   for (int p = 0; p < RP; ++p)
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(512) void orth_small_kernel(OrthArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         _Float16 h, l;
-        split(x[p][j][e] * inv, h, l);
+        split((float)(x[p][j][e] * inv), h, l);
         xh[p][j][e] = h;
         xl[p][j][e] = l;
       }
@@ -351,11 +351,11 @@ __global__ __launch_bounds__(256) void orth_scale_kernel(OrthArgs a) {
   double ss = 0.;
   for (int i = v0; i < a.parts; i += 64) ss += a.part[b * a.parts + i];
   for (int m = 1; m < 64; m <<= 1) ss += __shfl_xor(ss, m, 64);
-  const float inv = (float)((double)SX / (sqrt(ss) + (double)a.eps));
+  const double inv = (double)SX / (sqrt(ss) + (double)a.eps);  // of a small norm, past fp32
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int u = u0 + 4 * i;
-    const float y = u < nu && v0 < nv ? inv * x[i] : 0.f;
+    const float y = u < nu && v0 < nv ? (float)(inv * x[i]) : 0.f;
     if (a.flip) t[v0][u] = y;
     else t[u][v0] = y;
   }

@@ -219,3 +219,15 @@ def test_first_element_anywhere(r, c, dtype):
         torch.cuda.synchronize()
         check("orth offset", out, G, [MUON] * 5)
         assert (dst[:off] == 7).all() and (dst[off + 2 * r * c:] == 7).all()
+
+
+@pytest.mark.parametrize("scale", [1e-36, 1e-37, 1e-39])
+@pytest.mark.parametrize("r,c", [(30, 50), (140, 150)])
+def test_norms_near_the_smallest_numbers(r, c, scale):
+    """A norm whose reciprocal leaves fp32 (entries with few bits left, but exact as given), without
+    and with an eps as small."""
+    G = matrices(1, r, c, torch.float32, seed=12, scale=scale)
+    check(f"orth scale {scale}", run(G.to(DEV), eps=0.0), G, [MUON] * 5, 0.0)
+    tiny = torch.tensor(1e-39).item()
+    check(f"orth scale {scale} eps", run(G.to(DEV), eps=tiny), G, [MUON] * 5, tiny)
+    assert torch.equal(run(torch.zeros(2, r, c, device=DEV), eps=tiny), torch.zeros(2, r, c, device=DEV))
