@@ -290,7 +290,8 @@ tnt_status tnt_dbg_chunk_grads(const tnt_config* cfg, int32_t b, int32_t h, int3
  *  - q, k : [B][Hk][L][d_k], v, o : [B][H][L][d_v] (dtype), H a multiple of Hk: value
  *    heads h*H/Hk .. share key head h, and dq, dk are summed over them;
  *    g, lr : [B][H][L] fp32; S0, final_state : [n][H][d_k][d_v] fp32, n sequences.
- *  - g is the log of the decay factor, g <= 0; below -80 (-inf included) it acts as -80.
+ *  - g is the log of the decay factor; below -80 (-inf included) it acts as -80, above 0
+ *    the state grows, in every form alike.
  *    Keys are expected to have about unit norm and lr to lie in [0, 2): outside,
  *    the recurrence itself grows.
  *  - `strides` gives the element strides of every tensor (innermost elements

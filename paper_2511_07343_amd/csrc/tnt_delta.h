@@ -9,7 +9,7 @@
 //     O  = scale (e^c (Q S) + (D * Q K^T) (lr W))
 //     S' = e^(c_64) S + K^T (e^(c_64 - c) lr W)
 // Every exponent is a difference of a later and an earlier sum, so nothing
-// overflows however strong the decay.  Log decays are clamped at -80.
+// overflows however strong the decay (g > 0 grows the state as the recurrence does).  Log decays are clamped at -80.
 //
 // Precision.  States, gate gradients and everything on the way to them are
 // fp32, and are to be as exact as fp32 sums: an fp32 operand of an MFMA product
@@ -455,13 +455,10 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-// e^(x + y) of a difference of two such pairs
+// e^(x + y) of a difference of two such pairs.  Where a lies before b it may be infinite:
+// such places are masked by a choice, never by a factor of zero.
 __device__ __forceinline__ float exp_diff(const float2& a, const float2& b) {
   return expf((a.x - b.x) + (a.y - b.y));
-}
-// the same where a is at or after b; 1 elsewhere (to be masked), without a branch
-__device__ __forceinline__ float exp_decay(const float2& a, const float2& b) {
-  return expf(fminf((a.x - b.x) + (a.y - b.y), 0.f));
 }
 __device__ __forceinline__ float exp_pair(const float2& a) { return expf(a.x + a.y); }
 

@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256) void delta_dlocal_kernel(DeltaArgs a) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int key = 16 * w + c, qry = 16 * i + 4 * q + r;
-      const float d = a.scale * p[i][r] * exp_decay(cl[qry], cl[key]);
+      const float d = a.scale * p[i][r] * exp_diff(cl[qry], cl[key]);
       x[r] = key <= qry && qry < ch.n ? d : 0.f;
     }
     split4_store(x, Pl + w * 3072 + (i >> 1) * 1536 + lane * 8 + 4 * (i & 1));
@@ -495,7 +495,7 @@ __global__ __launch_bounds__(4 * DK) void delta_grads_kernel(DeltaArgs a) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int qi = 16 * i + 4 * q + r, kj = 16 * j + c;
-          const float d = exp_decay(cl[qi], cl[kj]);
+          const float d = exp_diff(cl[qi], cl[kj]);
           const float x = a.scale * d * tp[n][r];
           g[r] = qi > kj ? x : 0.f;
           if (qi == kj) diag[qi] = x;

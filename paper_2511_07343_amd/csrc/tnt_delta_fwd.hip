@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a) {
         for (int r = 0; r < 4; ++r) {
           const int row = 16 * w + 4 * q + r, col = 16 * j + c;
           float x = 0.f;
-          const float d = acc[j][r] * exp_decay(cl[row], cl[col]) * ll[BWD ? row : col];
+          const float d = acc[j][r] * exp_diff(cl[row], cl[col]) * ll[BWD ? row : col];
           if (row > col) x = d;
           Al[row * AP + col] = x;
         }
@@ -462,7 +462,7 @@ __global__ __launch_bounds__(256, 3) void delta_out_kernel(DeltaArgs a) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int key = 16 * j + 4 * q + r, qry = 16 * w + c;
-      const float d = a.scale * p[j][r] * exp_decay(cl[qry], cl[key]);
+      const float d = a.scale * p[j][r] * exp_diff(cl[qry], cl[key]);
       x[r] = key <= qry ? d : 0.f;
     }
     split4_store(x, Pl + w * 3072 + (j >> 1) * 1536 + lane * 8 + 4 * (j & 1));

@@ -426,3 +426,22 @@ def test_slices_of_a_sequence():
         g = tnt.delta_backward(cfg, cut, cut["dO"], saved=saved)
         w = tnt.delta_backward(cfg, whole, whole["dO"], saved=wsaved)
         assert torch.equal(o, wo) and all(torch.equal(g[n], w[n]) for n in w)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_growing_states(dtype):
+    """g above 0: the state grows by e^g, in the chunked forward, the backward and token by token."""
+    def g(B, H, L, gen):
+        x = 0.03 * torch.randn(B, H, L, generator=gen)
+        x[:, 1] = 0.02
+        return x
+
+    x = make(1, 2, 150, 64, 64, dtype=dtype, seed=51, S0=True, g=g)
+    cfg = tnt.DeltaConfig(B=1, H=2, L=150, dk=64, dv=64, dtype=int(dtype == torch.bfloat16))
+    got, want = both(cfg, x)
+    compare(f"delta growing {dtype}", got, want)
+    d = gpu(x)
+    state = d["S0"].clone()
+    o = tnt.delta_step(cfg, {n: d[n] for n in ("q", "k", "v", "g", "lr")}, state)
+    torch.cuda.synchronize()
+    compare(f"delta growing steps {dtype}", dict(o=o, state=state), dict(o=want["o"], state=want["state"]))
