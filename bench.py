@@ -178,19 +178,27 @@ LAUNCH_SOURCES = {
 MFMA_FILE = {2: "mfma_ops_pretrain_B4H8L8192.txt"}
 
 
-def all_sources_hash():
+# sources of operators that the layer's step does not run
+OTHER_OPERATORS = ("tnt_delta", "tnt_orth")
+
+
+def layer_sources():
+    return sorted(fn for fn in os.listdir(os.path.join(ROOT, "paper_2511_07343_amd", "csrc"))
+                  if not fn.startswith(OTHER_OPERATORS))
+
+
+def layer_sources_hash():
     import hashlib
     h = hashlib.sha256()
-    d = os.path.join(ROOT, "paper_2511_07343_amd", "csrc")
-    for fn in sorted(os.listdir(d)):
-        with open(os.path.join(d, fn), "rb") as f:
+    for fn in layer_sources():
+        with open(os.path.join(ROOT, "paper_2511_07343_amd", "csrc", fn), "rb") as f:
             h.update(f.read())
     return h.hexdigest()[:16]
 
 
 def measured_mfma(workload):
     """MFMA FLOPs per step counted by rocprofv3 (committed summary), or None
-    once any kernel source changed since the count was taken."""
+    once any source of the layer changed since the count was taken."""
     fn = MFMA_FILE.get(workload)
     path = os.path.join(ROOT, "profiles", fn) if fn else None
     if not path or not os.path.exists(path):
@@ -199,7 +207,7 @@ def measured_mfma(workload):
         for line in f:
             t = line.split()
             if len(t) >= 6 and t[0] == "step" and t[1] == "sha256":
-                return float(t[5]) if t[2] == all_sources_hash() else None
+                return float(t[5]) if t[2] == layer_sources_hash() else None
     return None
 
 

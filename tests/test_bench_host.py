@@ -73,3 +73,13 @@ def test_local_carry_bytes_workload2():
     assert cb["alg_bytes"] == 128 * 32 * per_chunk == 640679936
     assert cb["spilled_state_bytes"] == 128 * 32 * 2 * 4 * 256 * 64 * 4
     assert bench.hbm_bytes(cfg, "local_carry") == cb["alg_bytes"]
+
+
+def test_mfma_count_covers_the_layers_sources():
+    """The counted MFMA FLOPs of a step stand for the sources that the layer is built from: every
+    launch's, and none of the operators beside it."""
+    files = bench.layer_sources()
+    assert not [f for f in files if f.startswith(("tnt_delta", "tnt_orth"))]
+    for lab in bench.LAUNCH_SOURCES:
+        assert set(bench.LAUNCH_SOURCES[lab]) <= set(files)
+    assert {"tnt_abi.cpp", "tnt_step.hip", "tnt_kernels.h"} <= set(files)
