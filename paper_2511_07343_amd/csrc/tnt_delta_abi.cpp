@@ -114,9 +114,11 @@ tnt_status begin(const tnt_delta_config* c, const tnt_delta_strides* s, bool bwd
   a.sv = a.so = a.sdO = a.sdv = contiguous(c->H, c->L, c->d_v);
   a.sg = a.sl = a.sdg = a.sdl = contiguous(c->H, c->L, 0);
   if (s) {
-    a.sq = str_of(s->q); a.sk = str_of(s->k); a.sv = str_of(s->v); a.so = str_of(s->o);
+    a.sq = str_of(s->q); a.sk = str_of(s->k); a.sv = str_of(s->v);
     a.sg = str_of(s->g); a.sl = str_of(s->lr);
-    if (bwd) {
+    if (!bwd) {
+      a.so = str_of(s->o);
+    } else {
       a.sdO = str_of(s->dO); a.sdq = str_of(s->dq); a.sdk = str_of(s->dk); a.sdv = str_of(s->dv);
       a.sdg = str_of(s->dg); a.sdl = str_of(s->dlr);
     }

@@ -187,3 +187,14 @@ def test_element_wise_tensors_at_any_element(n, off, ok):
         got = tnt.tnt_delta_step(c, tnt.tnt_delta_strides(*s), P, P, P, at("g"), at("lr"), P, 8, at("slots"), P,
                                  stream=0)
         assert got == (7 if ok else 5)
+
+
+def test_strides_that_are_not_read():
+    """The backward has no output o, so whatever stands in its strides is not looked at."""
+    c, s = cfg(), []
+    for name in ("q", "k", "v", "v", "g", "g", "v", "q", "k", "v", "g", "g"):
+        s += torch.empty(c.shape(name), device="meta").stride()[:3]
+    for junk in (0, -3, 65, 1 << 40):
+        s[9:12] = [junk] * 3
+        assert bwd(c, tnt.tnt_delta_strides(*s), ws=0) == 4
+        assert fwd(c, tnt.tnt_delta_strides(*s), ws=0) in (3, 5, 7)
