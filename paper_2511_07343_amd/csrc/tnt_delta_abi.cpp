@@ -1,6 +1,7 @@
 // C ABI of the gated delta rule: validation, workspace layout and launch sequence.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "../../include/tnt.h"
@@ -30,15 +31,18 @@ struct Plan {
       sv_w, sv_s, saved, fwd, bwd, bwd_re;
 };
 
-// 0: fits the grids of the launches
+constexpr int64_t MAX_THREADS = UINT32_MAX;  // of a launch
+
+// false: does not fit the grids of the launches
 bool plan_of(const tnt_delta_config* c, Plan* p) {
   p->DK = c->d_k <= 32 ? 32 : c->d_k <= 64 ? 64 : 128;
   p->dvt = (c->d_v + 15) / 16;
   p->nseq = c->n_seq ? c->n_seq : c->B;
   p->nc = (int)(((int64_t)c->L + DC - 1) / DC);
   const int64_t slots = c->n_seq ? (int64_t)c->L / DC + c->n_seq : (int64_t)c->B * p->nc;
-  const int64_t lim = INT32_MAX / 8;
-  if (slots * c->H > lim || ((int64_t)p->nseq * c->H + 7) * p->dvt > lim) return false;
+  // threads of the passes over chunks (grads: 4 DK a key head) and of the chains
+  const int64_t chunk = std::max<int64_t>(256 * (int64_t)c->H, 4 * p->DK * (int64_t)c->Hk);
+  if (slots > MAX_THREADS / chunk || ((int64_t)p->nseq * c->H + 7) * p->dvt > MAX_THREADS / 256) return false;
   p->slots = (int)slots;
   p->pitch = c->d_v <= 32 ? 32 : c->d_v <= 64 ? 64 : 128;
   p->chunks = (size_t)slots * c->H;
@@ -276,7 +280,7 @@ tnt_status tnt_delta_step(const tnt_delta_config* cfg, const tnt_delta_strides* 
     if (p && misaligned(p)) return TNT_ERR_ALIGN;
   for (const void* p : {(const void*)g, (const void*)lr, (const void*)slots})
     if (p && split_element(p)) return TNT_ERR_ALIGN;
-  if ((int64_t)cfg->B * cfg->H * 8 > INT32_MAX / 8) return TNT_ERR_UNSUPPORTED;
+  if ((int64_t)cfg->B * cfg->H * ((cfg->d_v + 31) / 32) > MAX_THREADS / 64) return TNT_ERR_UNSUPPORTED;
   DeltaStepArgs a{};
   a.q = q; a.k = k; a.v = v; a.g = g; a.lr = lr; a.state = state; a.slot = slots; a.o = o;
   a.B = cfg->B; a.H = cfg->H; a.per = cfg->H / cfg->Hk; a.T = cfg->L;

@@ -198,3 +198,16 @@ def test_strides_that_are_not_read():
         s[9:12] = [junk] * 3
         assert bwd(c, tnt.tnt_delta_strides(*s), ws=0) == 4
         assert fwd(c, tnt.tnt_delta_strides(*s), ws=0) in (3, 5, 7)
+
+
+def test_launches_past_the_grid_are_refused():
+    """A launch holds fewer than 2^32 threads: more (sequence, head) tiles or chunks are refused before
+    anything is enqueued."""
+    c, s = cfg(B=1 << 20, H=31, Hk=31, L=1, dk=128, dv=128), []
+    for name in ("q", "k", "v", "v", "g", "g"):
+        s += torch.empty(c.shape(name), device="meta").stride()[:3]
+    s[9] = 0  # (a broadcast output: the call would end there)
+    assert tnt.tnt_delta_step(c, tnt.tnt_delta_strides(*s), P, P, P, P, P, P, 1 << 20, None, P, stream=0) == 3
+    for big in (dict(B=1 << 20, H=31, Hk=31, L=0, dk=64, dv=16), dict(B=1 << 20, H=17, Hk=17, L=1, dk=8, dv=8)):
+        assert fwd(cfg(**big), ws=0) == 3 and bwd(cfg(**big), ws=0) == 3
+    assert fwd(cfg(B=1 << 19, H=16, Hk=16, L=1, dk=8, dv=8), ws=0) == 4
