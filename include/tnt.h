@@ -343,8 +343,9 @@ tnt_status tnt_delta_fwd(const tnt_delta_config* cfg, const tnt_delta_strides* s
                          size_t ws_bytes, void* stream);
 
 /* Backward: gradients of sum(dO * o) + sum(dfinal * final_state).  dfinal and dS0 may be
- * NULL.  saved: what tnt_delta_fwd wrote for the same inputs, or NULL to recompute it
- * (ws_bytes then covers TNT_WS_BWD_RECOMPUTE). */
+ * NULL.  saved: what tnt_delta_fwd wrote for the same inputs and configuration (it names
+ * neither itself, and only its size is checked), or NULL to recompute it (ws_bytes then
+ * covers TNT_WS_BWD_RECOMPUTE). */
 tnt_status tnt_delta_bwd(const tnt_delta_config* cfg, const tnt_delta_strides* strides,
                          const void* q, const void* k, const void* v, const float* g,
                          const float* lr, const int32_t* seq_start, const float* S0,

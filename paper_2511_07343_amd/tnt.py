@@ -555,6 +555,9 @@ def delta_backward(cfg: DeltaConfig, x: Dict[str, torch.Tensor], dO: torch.Tenso
     for n, t in (("workspace", workspace), ("saved", saved)):
         if t is not None:
             _place(dev, n, t)
+    if saved is not None and _nbytes(saved, None) != max(16, cfg.size("saved")):
+        raise ValueError(f"saved: expected {cfg.size('saved')} bytes, got {_nbytes(saved, None)}: "
+                         "of another configuration")
     if _elsewhere(stream, dev):
         return _on_stream(stream, dev, (*x.values(), dO, saved, dfinal, workspace),
                           lambda: delta_backward(cfg, x, dO, saved, dfinal, workspace))

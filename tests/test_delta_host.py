@@ -211,3 +211,19 @@ def test_launches_past_the_grid_are_refused():
     for big in (dict(B=1 << 20, H=31, Hk=31, L=0, dk=64, dv=16), dict(B=1 << 20, H=17, Hk=17, L=1, dk=8, dv=8)):
         assert fwd(cfg(**big), ws=0) == 3 and bwd(cfg(**big), ws=0) == 3
     assert fwd(cfg(B=1 << 19, H=16, Hk=16, L=1, dk=8, dv=8), ws=0) == 4
+
+
+def test_saved_buffer_of_another_configuration(monkeypatch):
+    """A saved buffer of another size was written for other shapes, a larger one too."""
+    monkeypatch.setattr(tnt, "_elsewhere", lambda stream, dev: False)
+    monkeypatch.setattr(tnt, "_current", lambda dev: 0)
+    monkeypatch.setattr(tnt, "tnt_delta_bwd", lambda *a, **kw: 0)
+    c = cfg(B=1, H=2, Hk=1, L=70, dk=8, dv=8)
+    x = {n: torch.zeros(c.shape(n), dtype=c.io if n in "qkv" else torch.float32)
+         for n in ("q", "k", "v", "g", "lr")}
+    dO = torch.zeros(c.shape("v"), dtype=c.io)
+    saved = lambda k: torch.empty(k.size("saved"), dtype=torch.uint8)
+    tnt.delta_backward(c, x, dO, saved=saved(c))
+    for other in (dict(L=200), dict(L=60), dict(dk=40), dict(dv=40), dict(H=4)):
+        with pytest.raises(ValueError, match="saved"):
+            tnt.delta_backward(c, x, dO, saved=saved(cfg(**{**dict(B=1, H=2, Hk=1, L=70, dk=8, dv=8), **other})))
