@@ -34,8 +34,8 @@ struct OrthArgs {
   _Float16 *A, *B;   // [n][2][mp][lm]
 };
 
-// one workgroup a matrix: fits its registers
-bool orth_small(int m, int k);
+// one workgroup a matrix: fits its registers, and is the faster form
+bool orth_small(int n, int m, int k);
 hipError_t launch_orth_small(const OrthArgs& a, hipStream_t st);
 hipError_t launch_orth_large(const OrthArgs& a, hipStream_t st);
 

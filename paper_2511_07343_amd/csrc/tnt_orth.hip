@@ -591,9 +591,13 @@ hipError_t small(const OrthArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// A shorter side of 65 to 128 fits too (256 registers of eight waves, with spills), but one
-// CU a matrix is then the slower form: 32 matrices of 128 x 512 in 212 us.
-bool orth_small(int m, int k) { return m <= 64 && k <= 1024; }
+// Shorter sides of up to 64.  (65 to 128 fit too, in 256 registers of eight waves with spills, but
+// one CU a matrix is then the slower form: 32 matrices of 128 x 512 in 212 us against 126.)  Longer
+// sides of up to 512, or 1024 with a shorter one of up to 32, take less than the tiles' 17
+// launches at any number of matrices (one of 64 x 512: 59 us against 86, 16 x 1024: 38 / 107).
+// 33 to 64 by 513 to 1024 spill, 135 to 175 us for up to 64 matrices, where the tiles take 88
+// to 118 for 16, 108 to 155 for 48, 127 to 168 for 64 and 600 to 1000 for 256 (here 184 to 222).
+bool orth_small(int n, int m, int k) { return m <= 64 && k <= (m <= 32 || n > 48 ? 1024 : 512); }
 
 hipError_t launch_orth_small(const OrthArgs& a, hipStream_t st) {
   const int rp = a.k <= 256 ? 1 : a.k <= 512 ? 2 : 4;

@@ -69,7 +69,7 @@ Lay lay_of(const tnt_orth_config* c) {
   l.k = std::max(c->rows, c->cols);
   // (whose elements are addressed by 32-bit offsets from the matrix)
   const int64_t apart = std::max(std::max(c->g_row, c->out_row), (int64_t)c->cols);
-  l.small = orth_small(l.m, l.k) && apart < INT32_MAX / 1024;
+  l.small = orth_small(c->n, l.m, l.k) && apart < INT32_MAX / 1024;
   if (l.small) return l;
   l.mp = (l.m + ORTH_TILE - 1) / ORTH_TILE * ORTH_TILE;
   l.kp = (l.k + ORTH_TILE - 1) / ORTH_TILE * ORTH_TILE;

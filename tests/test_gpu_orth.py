@@ -231,3 +231,11 @@ def test_norms_near_the_smallest_numbers(r, c, scale):
     tiny = torch.tensor(1e-39).item()
     check(f"orth scale {scale} eps", run(G.to(DEV), eps=tiny), G, [MUON] * 5, tiny)
     assert torch.equal(run(torch.zeros(2, r, c, device=DEV), eps=tiny), torch.zeros(2, r, c, device=DEV))
+
+
+@pytest.mark.parametrize("n,r,c", [(49, 64, 1024), (50, 33, 513), (52, 700, 50), (1, 64, 1000), (2, 600, 33)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_longer_sides_of_513_to_1024(n, r, c, dtype):
+    """Both sides of the rule: many matrices in a workgroup each, a few of them in tiles."""
+    G = matrices(n, r, c, dtype, seed=n + r)
+    check(f"orth {n}x{r}x{c} {dtype}", run(G.to(DEV)), G, [MUON] * 5)

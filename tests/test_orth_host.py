@@ -159,3 +159,12 @@ def test_matrices_at_any_element(dtype, off, ok):
     for g, out in ((P + off, P), (P, P + off)):
         assert tnt.tnt_orth_update(cfg.c, None, g, out, P, ws_bytes=0, stream=0) == (4 if ok else 5)
     assert tnt.tnt_orth_update(cfg.c, None, P, P, P + 8, ws_bytes=0, stream=0) == 5
+
+
+@pytest.mark.parametrize("n,r,c,tiles", [
+    (1, 33, 513, True), (48, 64, 1024, True), (48, 900, 40, True), (49, 64, 1024, False), (300, 33, 513, False),
+    (1, 32, 1024, False), (1, 64, 512, False), (1, 65, 100, True), (1, 10, 1025, True)])
+def test_which_form(n, r, c, tiles):
+    """One workgroup a matrix needs no workspace; it serves shorter sides of up to 64, longer ones of up
+    to 512, and to 1024 where the shorter is at most 32 or there are matrices for a fifth of the card."""
+    assert (tnt.tnt_orth_workspace_size(tnt.OrthConfig(n=n, rows=r, cols=c)) > 16) == tiles
