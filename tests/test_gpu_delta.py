@@ -445,3 +445,48 @@ def test_growing_states(dtype):
     o = tnt.delta_step(cfg, {n: d[n] for n in ("q", "k", "v", "g", "lr")}, state)
     torch.cuda.synchronize()
     compare(f"delta growing steps {dtype}", dict(o=o, state=state), dict(o=want["o"], state=want["state"]))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dk,dv", [(16, 24), (32, 32), (64, 64), (96, 80), (128, 128)])
+def test_shared_heads_of_every_size(dk, dv, dtype):
+    """Value heads that share keys at every padded key size and type, over three chunks, packed rows from
+    carried states among them."""
+    flag = int(dtype == torch.bfloat16)
+    x = make(2, 6, 150, dk, dv, Hk=2, dtype=dtype, seed=dk, S0=True)
+    cfg = tnt.DeltaConfig(B=2, H=6, Hk=2, L=150, dk=dk, dv=dv, dtype=flag, scale=0.3)
+    compare(f"delta shared {dk}x{dv} {dtype}", *both(cfg, x, tokens_first=True))
+    starts = [0, 0, 67, 68, 150]
+    x = make(1, 4, 150, dk, dv, Hk=1, dtype=dtype, n=4, seed=dv, S0=True)
+    cfg = tnt.DeltaConfig(B=1, H=4, Hk=1, L=150, dk=dk, dv=dv, n_seq=4, dtype=flag)
+    compare(f"delta shared packed {dk}x{dv} {dtype}", *both(cfg, x, starts=starts))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dk,dv,L", [(128, 128, 390), (104, 64, 448), (64, 128, 390), (32, 16, 384)])
+def test_several_chunks_of_every_size(dk, dv, L, dtype):
+    """Six and seven chunks: every turn of the chains' buffers, an even and an odd number of chunks."""
+    x = make(1, 2, L, dk, dv, dtype=dtype, seed=dk + L, S0=True)
+    cfg = tnt.DeltaConfig(B=1, H=2, L=L, dk=dk, dv=dv, dtype=int(dtype == torch.bfloat16), scale=0.2)
+    compare(f"delta chunks {dk}x{dv} L{L} {dtype}", *both(cfg, x))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dk,dv", [(40, 24), (128, 128)])
+def test_saved_buffer_and_workspaces_of_nan(dk, dv, dtype):
+    """Nothing is read that the calls have not written: saved buffer, forward's and both backwards'
+    workspaces filled with NaN beforehand."""
+    x = make(1, 4, 200, dk, dv, Hk=2, n=3, dtype=dtype, seed=61, S0=True)
+    cfg = tnt.DeltaConfig(B=1, H=4, Hk=2, L=200, dk=dk, dv=dv, n_seq=3, dtype=int(dtype == torch.bfloat16))
+    d = dict(gpu(x), seq_start=torch.tensor([0, 70, 71, 200], dtype=torch.int32, device=DEV))
+    o, saved, fin = tnt.delta_forward(cfg, d, final_state=True)
+    g = tnt.delta_backward(cfg, d, d["dO"], saved=saved, dfinal=d["dfinal"])
+    nan = lambda kind: torch.full((cfg.size(kind),), 255, dtype=torch.uint8, device=DEV)
+    o2, fin2, saved2 = torch.empty_like(o), torch.empty_like(fin), nan("saved")
+    assert tnt.tnt_delta_fwd(cfg, None, d["q"], d["k"], d["v"], d["g"], d["lr"], d["seq_start"], d["S0"], o2, fin2,
+                             saved2, nan(tnt.TNT_WS_FWD)) == 0
+    for kept, kind in ((saved2, tnt.TNT_WS_BWD), (None, tnt.TNT_WS_BWD_RECOMPUTE)):
+        g2 = tnt.delta_backward(cfg, d, d["dO"], saved=kept, dfinal=d["dfinal"], workspace=nan(kind))
+        torch.cuda.synchronize()
+        assert all(torch.equal(g[n], g2[n]) for n in g)
+    assert torch.equal(o, o2) and torch.equal(fin, fin2)

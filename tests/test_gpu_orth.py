@@ -239,3 +239,25 @@ def test_longer_sides_of_513_to_1024(n, r, c, dtype):
     """Both sides of the rule: many matrices in a workgroup each, a few of them in tiles."""
     G = matrices(n, r, c, dtype, seed=n + r)
     check(f"orth {n}x{r}x{c} {dtype}", run(G.to(DEV)), G, [MUON] * 5)
+
+
+@pytest.mark.parametrize("n,r,c", [(4, 64, 256), (2, 300, 31), (2, 65, 300), (3, 500, 510), (1, 1030, 700), (2, 129, 640)])
+def test_fp32_accuracy(n, r, c):
+    """Operands of 22 bits, each product's rounding independent: 2^-23 of its norm, sqrt(15) of them, the
+    amplification of 25; one term less anywhere is 2^-12 in its place."""
+    G = matrices(n, r, c, torch.float32, seed=n * r)
+    out = run(G.to(DEV))
+    for i in range(n):
+        want = O.orthogonalise(G[i], [MUON] * 5)
+        e = ((out[i].double().cpu() - want).norm() / want.norm()).item()
+        assert check_err(f"orth fp32 {n}x{r}x{c}", f"out[{i}]", e, 25 * 15 ** 0.5 * 2.0 ** -23), (i, e)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_many_matrices_of_many_tiles(dtype):
+    """Ragged sides of several tiles, more workgroups than the card takes at once; matrices at the ends and
+    in between."""
+    G = matrices(64, 500, 510, dtype, seed=13)
+    out = run(G.to(DEV))
+    pick = [0, 7, 31, 63]
+    check(f"orth many {dtype}", out[pick], G[pick], [MUON] * 5)
