@@ -255,7 +255,6 @@ __device__ __forceinline__ void mma_terms_2(f4 (&acc)[N], const Fr<NA> (&a)[N], 
 // Contraction indices of a lane's 8 elements in a step of 32: k0 + 4q + (0..3) and
 // k0 + 16 + 4q + (0..3), q = lane / 16: the order in which two stacked accumulator
 // tiles hold their rows, so that tiles serve as operands without a move.
-__device__ __forceinline__ float elem(float x) { return x; }
 __device__ __forceinline__ Fr<1> frag_of(const bf16x4& a, const bf16x4& b) {
   Fr<1> f;
   f.p[0] = join(a, b);
@@ -380,7 +379,7 @@ __device__ __forceinline__ bool chain_unit(const DeltaArgs& a, int& seq, int& h,
 // contractions.  Tiles 0, 1 of a lower triangular factor have one step of 32, tiles 2, 3
 // two; two waves take one of each.
 template <int NW> __device__ __forceinline__ int chain_tile(int w, int i) {
-  return NW == 4 ? w : NW == 2 ? (i ? 3 - w : w) : i;
+  return NW == 4 ? w : i ? 3 - w : w;
 }
 
 // T's rows of one wave (RT tiles) times the chunk's 64 rows in LDS planes: chains of three

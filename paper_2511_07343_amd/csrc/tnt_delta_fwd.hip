@@ -9,9 +9,9 @@ constexpr int AP = 68;  // floats a row of the 64x64 matrices in LDS (16-byte ro
 
 // ---------------------------------------------------------------------------------
 // Packed sequences: seq_start [nseq + 1] on the device -> the first chunk slot of every
-// sequence and the table of slots.  One workgroup: a scan of the chunk counts, then each
-// slot finds its sequence by bisection.  Starts are clamped into [0, L] and made
-// non-decreasing, so that no list of starts leads outside the tensors.
+// sequence and the table of slots.  One workgroup, a thread a sequence: a scan of the chunk
+// counts, then each thread writes its sequence's slots in turn.  Starts are clamped into
+// [0, L] and made non-decreasing, so that no list of starts leads outside the tensors.
 // ---------------------------------------------------------------------------------
 __global__ __launch_bounds__(1024) void delta_plan_kernel(const int* start, int nseq, int L, int slots,
                                                           int* first, int4* table) {
@@ -313,11 +313,11 @@ __global__ __launch_bounds__(64 * ChainShape<DK>::NW, sizeof(E) == 2 && DK > 32 
 void delta_chain_kernel(DeltaArgs a) {
   typedef ChainLoad<E, DK> X;
   constexpr int NW = X::NW, RT = X::RT, SR = X::SR;
-  __shared__ __attribute__((aligned(16))) f4 part[NW > 1 ? NW * 256 : 1];
+  __shared__ __attribute__((aligned(16))) f4 part[NW * 256];
   __shared__ __attribute__((aligned(16))) __bf16 Ep[3072], Up[3072];
   int seq, h, ct;
   if (!chain_unit(a, seq, h, ct)) return;
-  const int tid = threadIdx.x, lane = tid & 63, w = NW > 1 ? wave_id_uniform() : 0;
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_id_uniform();
   const int q = lane >> 4, col = 16 * ct + (lane & 15);
   constexpr int pitch = PV;
   f4 S[SR];
@@ -342,16 +342,14 @@ void delta_chain_kernel(DeltaArgs a) {
     const auto sf = StateOp<SR>::of(S);
     f4 ks[4] = {zero4(), zero4(), zero4(), zero4()};
     mma_terms_n(ks, cur.kf, sf);
-    if (NW > 1) {
 #pragma unroll
-      for (int rt = 0; rt < 4; ++rt) part[(w * 4 + rt) * 64 + lane] = ks[rt];
-      lds_barrier();
-    }
+    for (int rt = 0; rt < 4; ++rt) part[(w * 4 + rt) * 64 + lane] = ks[rt];
+    lds_barrier();
     f4 x[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
       const int rt = chain_tile<NW>(w, i);
-      x[i] = NW > 1 ? part[rt * 64 + lane] : ks[i];
+      x[i] = part[rt * 64 + lane];
 #pragma unroll
       for (int o = 1; o < NW; ++o) x[i] += part[(o * 4 + rt) * 64 + lane];
     }
