@@ -502,19 +502,22 @@ __global__ __launch_bounds__(4 * DK) void delta_grads_kernel(DeltaArgs a) {
           m[r] = qi > kj ? -ll[qi] * d * ta[n][r] : 0.f;
         }
         // as rows of the keys (lane's column c), contraction over the queries 4q + r
-        split4_store(g, Gk + j * 3072 + (i >> 1) * 1536 + lane * 8 + 4 * (i & 1));
-        if (i != j) split4_store(m, Mf + j * 3072 + (i >> 1) * 1536 + lane * 8 + 4 * (i & 1));
+        uint32_t tg[3][2], tm[3][2];
+        split_n(g, tg);
+        split_n(m, tm);
+        terms4_store(tg, Gk + j * 3072 + (i >> 1) * 1536 + lane * 8 + 4 * (i & 1));
+        if (i != j) terms4_store(tm, Mf + j * 3072 + (i >> 1) * 1536 + lane * 8 + 4 * (i & 1));
         // the other way: row 4q + r, contraction index c of tile j: lane 16 (c / 4) + row
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int rr = 4 * q + r, step = (j >> 1) * 1536, el = 4 * (j & 1);
           const int at = step + (16 * (c >> 2) + rr) * 8 + el + (c & 3);
-          split_put(g[r], Gq + i * 3072 + at);
+          terms4_put(tg, r, Gq + i * 3072 + at);
           // of a diagonal tile of M + M^T the lane with row > column writes both places, the
           // lane on the diagonal its zero
           if (i != j || rr >= c) {
-            split_put(m[r], Mf + i * 3072 + at);
-            if (i == j) split_put(m[r], Mf + i * 3072 + step + (16 * (rr >> 2) + c) * 8 + el + (rr & 3));
+            terms4_put(tm, r, Mf + i * 3072 + at);
+            if (i == j) terms4_put(tm, r, Mf + i * 3072 + step + (16 * (rr >> 2) + c) * 8 + el + (rr & 3));
           }
         }
         __builtin_amdgcn_sched_barrier(0);

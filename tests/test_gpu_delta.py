@@ -490,3 +490,19 @@ def test_saved_buffer_and_workspaces_of_nan(dk, dv, dtype):
         torch.cuda.synchronize()
         assert all(torch.equal(g[n], g2[n]) for n in g)
     assert torch.equal(o, o2) and torch.equal(fin, fin2)
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_errors_of_both_signs(d):
+    """Sums of positive terms in fp32, o = S0^T q.  What the three terms of an operand leave out is below
+    2^-23 of a product and of either sign, and so are the sums' roundings, at most 2^-24 each: over the
+    2048 outputs and more their mean is far below 2^-26, where products left out with one sign have
+    2^-25."""
+    gen = torch.Generator().manual_seed(3)
+    r = lambda *s: torch.rand(*s, generator=gen) + 0.1
+    x = dict(q=r(1, 64, 1, d), k=r(1, 64, 1, d), v=r(1, 64, 1, d), g=torch.zeros(1, 64, 1),
+             lr=torch.zeros(1, 64, 1), S0=r(1, 64, d, d))
+    want = (x["q"][:, :, 0, :, None].double() * x["S0"].double()).sum(2)
+    o, _, _ = tnt.delta_forward(tnt.DeltaConfig(B=1, H=64, L=1, dk=d, dv=d, dtype=0), gpu(x), save=False)
+    mean = ((o[:, :, 0].double().cpu() - want) / want).mean().item()
+    assert check_err("delta mean error", f"o {d}", abs(mean), 2.0 ** -26), mean
