@@ -371,8 +371,10 @@ tnt_status tnt_delta_step(const tnt_delta_config* cfg, const tnt_delta_strides* 
  *    every step.  They must keep the singular values that start in [0, 1] at or below 4
  *    and b A + c A^2 at or below 64 in norm (TNT_ERR_ARG): the products hold their
  *    operands in 16 bits at fixed scales.
- *  - Everything is computed to fp32 accuracy, whatever the matrices' type and sizes;
- *    outputs are rounded once.
+ *  - Everything is computed to the accuracy of fp32 sums in the matrix's norm, whatever its
+ *    type and size; outputs are rounded once.  The entries of a matrix share one scale
+ *    of 22 bits: rows 10^-2 of the others keep fp32's accuracy, rows 10^-4 of them
+ *    come out up to 8e-6 off, rows 10^-6 of them up to 8e-4.
  *  - A zero matrix gives zeros (eps > 0); a NaN or infinite entry spoils its own matrix
  *    alone.  Any sizes from 1 to 32768; matrices and rows begin at any element; out may
  *    be G. */

@@ -8,9 +8,11 @@
 //     o = scale (e^g S^T q + lr (k.q) e),   e = v - e^g S^T k
 // both contractions are over the entering state and run in one pass.  Bound by the
 // state's bytes, read and written once a call, past the caches: between two tokens of a
-// sequence lie the other layers' states.  248 sequences of 16 heads at 128 x 128, 523 MB,
-// with other states in between: 116 us (4.5 TB/s; a large copy reaches 5.1), 126 through
-// the caches.  Called again at once: 112, and 98 through the caches.  A few sequences
+// sequence lie the other layers' states.  248 sequences of 16 heads at 128 x 128, 260 MB
+// read and written: 117 us (4.5 TB/s; a large copy reaches 5.1).  Past the caches / through
+// them, us a launch in a graph, with three other pools in between or (again) the same one at
+// once: 0.5 MB 4.9 / 4.9, 8 MB 5.9 / 6.3 (5.9 / 6.1), 34 MB 14.6 / 15.6 (12.2 / 13.4), 67 MB
+// 28 / 31 (27 / 31), 134 MB 56 / 66 (56 / 53), 260 MB 105 / 121 (104 / 109).  A few sequences
 // cost a launch.
 #include "tnt_delta.h"
 
