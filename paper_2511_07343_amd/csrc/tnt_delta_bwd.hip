@@ -103,10 +103,11 @@ __global__ __launch_bounds__(256) void delta_dlocal_kernel(DeltaArgs a) {
 // Every product takes its right operand from the registers of the one before (accumulator
 // tiles as they stand), so a chunk needs no LDS and no barrier; each set of fragments is
 // requested for the next chunk as soon as this one has used it.  108 MFMAs a chunk at
-// dk 64, 180 at 128; bound by the instructions of a wave alone on its SIMD (2.0 us a chunk
-// of 32 x 4 column tiles at dk 64, 2.9 us of 16 x 8 at 128).  Cut by rows over four waves
-// as the forward's chain is, it took 2.1 and 2.9 us with few tiles and a third longer with
-// many (1408 tiles of 23 chunks at 128: 339 us here, 454 us so).
+// dk 64, 180 at 128; bound by the instructions of a wave alone on its SIMD: 2.0 us a chunk
+// of 32 x 4 column tiles at dk 64, 3.1 us of 16 x 8 at 128, issuing in 74 and 65 % of its
+// cycles.  Cut by rows over four waves as the forward's chain is, it took 2.1 and 2.9 us
+// with few tiles (2.0 and 2.9 here at the time) and a third longer with many (1408 tiles of
+// 23 chunks at 128: 454 us, 339 here).
 // ---------------------------------------------------------------------------------
 template <typename E, int DK, int PV>
 __global__ __launch_bounds__(64) void delta_bchain_kernel(DeltaArgs a) {
@@ -277,7 +278,10 @@ __global__ __launch_bounds__(64) void delta_bchain_kernel(DeltaArgs a) {
 // are taken 32 at a time: the waves split the rows of U, dR and dO into LDS, where they
 // serve as rows (dq, dk) and as columns (dqk, M); a wave takes two row tiles of two
 // column tiles of the keys, so that a state's fragment is split by two waves only and a
-// row fragment read by a quarter of them.
+// row fragment read by a quarter of them.  At dk 128 (1.38 ms for 16 x 32768 tokens) the waves
+// wait for memory, LDS and barriers in 57 % of their cycles and issue in 19 %, with one
+// workgroup a CU and 0.64 of 1.05 GB written spilled registers; at dk 64 (0.36 ms, 32 x 8192) 46
+// and 42 %.
 // ---------------------------------------------------------------------------------
 template <typename E, int DK> constexpr size_t grads_lds() {
   constexpr int NP = terms_of<E>();

@@ -344,7 +344,7 @@ __global__ __launch_bounds__(256) void orth_scale_kernel(OrthArgs a) {
   float x[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    // past the matrix: its last element (nu - 1 < 0 goes back from a tile of padding alone)
+    // past the matrix: its last element (every tile has one at least)
     x[i] = load_g(a, at0 + (int64_t)min(u0 + 4 * i, nu - 1) * a.gr + min(v0, nv - 1));
   }
   // every wave sums the parts, in the same order
@@ -399,6 +399,9 @@ __global__ __launch_bounds__(256) void orth_scale_kernel(OrthArgs a) {
 //   UPDATE  X^T <- a X^T + X^T B, both orientations (X in place: a tile reads its own
 //           place only; X^T, an operand, from one buffer to the other)
 //   LAST    the same into the caller's tensor
+// 4096 x 2048: UPDATE 131 us (the matrix units at work in 36 % of the cycles), GRAM 95 (23 %), SQUARE
+// 52 (20 %, 528 workgroups); a wave issues in 30 %, waits for issue in 35 % and for LDS and
+// barriers in a third.
 // ---------------------------------------------------------------------------------
 enum { GRAM = 0, SQUARE = 1, UPDATE = 2, LAST = 3 };
 
