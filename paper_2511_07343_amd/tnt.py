@@ -303,6 +303,9 @@ def forward(cfg: LayerConfig, x: Dict[str, torch.Tensor], save: bool = True,
             stream=None):
     """Run tnt_mem_fwd; returns (o, saved or None, final_state or None)."""
     dev = x["q"].device
+    if _elsewhere(stream, dev):
+        return _on_stream(stream, dev, (*x.values(), workspace),
+                          lambda: forward(cfg, x, save, final_state, workspace))
     o = torch.empty_like(x["q"])
     saved = _bytes(tnt_mem_saved_size(cfg), dev) if save else None
     fin = (torch.empty(cfg.B, cfg.H, 4, cfg.hid * cfg.d, dtype=torch.float32, device=dev)
@@ -310,7 +313,7 @@ def forward(cfg: LayerConfig, x: Dict[str, torch.Tensor], save: bool = True,
     if workspace is None:
         workspace = _bytes(tnt_mem_workspace_size(cfg, TNT_WS_FWD), dev)
     st = tnt_mem_fwd(cfg, x["q"], x["k"], x["v"], x["lr"], x["mom"], x["decay"], x["W1"],
-                     x["W2"], o, fin, saved, workspace, stream=stream)
+                     x["W2"], o, fin, saved, workspace)
     if st != 0:
         raise TntError(st, "tnt_mem_fwd")
     return o, saved, fin
@@ -321,6 +324,9 @@ def backward(cfg: LayerConfig, x: Dict[str, torch.Tensor], dO: torch.Tensor,
              stream=None) -> Dict[str, torch.Tensor]:
     """Run tnt_mem_bwd; returns the gradients of sum(dO * o)."""
     dev = x["q"].device
+    if _elsewhere(stream, dev):
+        return _on_stream(stream, dev, (*x.values(), dO, saved, workspace),
+                          lambda: backward(cfg, x, dO, saved, workspace))
     g = dict(dq=torch.empty_like(x["q"]), dk=torch.empty_like(x["k"]),
              dv=torch.empty_like(x["v"]), dlr=torch.empty_like(x["lr"]),
              dmom=torch.empty_like(x["mom"]), ddecay=torch.empty_like(x["decay"]),
@@ -330,7 +336,7 @@ def backward(cfg: LayerConfig, x: Dict[str, torch.Tensor], dO: torch.Tensor,
         workspace = _bytes(tnt_mem_workspace_size(cfg, kind), dev)
     st = tnt_mem_bwd(cfg, x["q"], x["k"], x["v"], x["lr"], x["mom"], x["decay"], x["W1"],
                      x["W2"], dO, saved, g["dq"], g["dk"], g["dv"], g["dlr"], g["dmom"],
-                     g["ddecay"], g["dW1"], g["dW2"], workspace, stream=stream)
+                     g["ddecay"], g["dW1"], g["dW2"], workspace)
     if st != 0:
         raise TntError(st, "tnt_mem_bwd")
     return g
@@ -342,9 +348,12 @@ def step_forward(cfg: LayerConfig, x: Dict[str, torch.Tensor], pieces, state=Non
     the given lengths (starting at token ``pos`` of ``x`` with ``state``, or
     from a fresh state); returns (o of the fed tokens [B,H,sum(pieces),d], state)."""
     dev = x["q"].device
+    if _elsewhere(stream, dev):
+        return _on_stream(stream, dev, (*x.values(), state),
+                          lambda: step_forward(cfg, x, pieces, state, pos))
     if state is None:
         state = _bytes(tnt_mem_state_size(cfg), dev)
-        st = tnt_mem_state_init(cfg, x["W1"], x["W2"], state, stream=stream)
+        st = tnt_mem_state_init(cfg, x["W1"], x["W2"], state)
         if st != 0:
             raise TntError(st, "tnt_mem_state_init")
     outs = []
@@ -357,8 +366,7 @@ def step_forward(cfg: LayerConfig, x: Dict[str, torch.Tensor], pieces, state=Non
         q, k, v = (cp(x[n][:, :, sl]) for n in ("q", "k", "v"))
         lr, mom, dec = (cp(x[n][..., sl]) for n in ("lr", "mom", "decay"))
         o = torch.empty_like(q)
-        st = tnt_mem_step(cfg, t0, T, q, k, v, lr, mom, dec, x["W1"], x["W2"], state, o,
-                          stream=stream)
+        st = tnt_mem_step(cfg, t0, T, q, k, v, lr, mom, dec, x["W1"], x["W2"], state, o)
         if st != 0:
             raise TntError(st, "tnt_mem_step")
         outs.append(o)

@@ -1,10 +1,10 @@
-"""The ``stream`` argument of the linear memory's and the update's calls: their buffers belong to that
+"""The ``stream`` argument of the layer's, the linear memory's and the update's calls: their buffers belong to that
 stream, and the results equal the calls' on the current stream, bit for bit, whatever the current
 stream is given meanwhile."""
 import pytest
 import torch
 
-from paper_2511_07343_amd import tnt
+from paper_2511_07343_amd import inputs, tnt
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -30,7 +30,15 @@ def calls():
             torch.cuda.synchronize()
         return tnt.delta_step(cfg, x, state, stream=stream), state
 
+    layer = inputs.WORKLOADS[0]
+    z = tnt.device_inputs(inputs.make_inputs(layer, 0), layer, device=DEV)
+    kept = tnt.forward(layer, z)[1]
+    torch.cuda.synchronize()
     return dict(
+        layer=lambda s: tnt.forward(layer, z, final_state=True, stream=s)[::2],
+        layer_backward=lambda s: tuple(tnt.backward(layer, z, z["dO"], saved=kept, stream=s).values()),
+        layer_recompute=lambda s: tuple(tnt.backward(layer, z, z["dO"], stream=s).values()),
+        layer_steps=lambda s: tnt.step_forward(layer, z, [100, 1, 60], stream=s)[:1],
         forward=lambda s: tnt.delta_forward(cfg, x, final_state=True, stream=s)[::2],
         backward=lambda s: tuple(tnt.delta_backward(cfg, x, dO, saved=saved, stream=s).values()),
         recompute=lambda s: tuple(tnt.delta_backward(cfg, x, dO, stream=s).values()),
@@ -38,7 +46,8 @@ def calls():
         update=lambda s: (tnt.orthogonalise(orth, G, stream=s),))
 
 
-@pytest.mark.parametrize("name", ["forward", "backward", "recompute", "step", "update"])
+@pytest.mark.parametrize("name", ["forward", "backward", "recompute", "step", "update", "layer", "layer_backward",
+                                  "layer_recompute", "layer_steps"])
 @pytest.mark.parametrize("raw", [False, True])
 def test_a_given_stream(name, raw, monkeypatch):
     call = calls()[name]
@@ -59,7 +68,7 @@ def test_a_given_stream(name, raw, monkeypatch):
     assert torch.cuda.current_stream() == torch.cuda.default_stream() and len(held) == 200
 
 
-@pytest.mark.parametrize("name", ["forward", "backward", "step", "update"])
+@pytest.mark.parametrize("name", ["forward", "backward", "step", "update", "layer", "layer_backward", "layer_steps"])
 def test_another_current_device(name, monkeypatch):
     """Tensors of a device that is not the current one: the library's launches go to the current device,
     so the tensors' is made current first."""
