@@ -235,3 +235,23 @@ def test_workspace_of_unpadded_global_chunks():
     for kw in (dict(d=16, hid=32), dict(d=64, hid=256), dict(d=16, hid=32, dtype=BF16)):
         for a, b in zip(sizes(130, **kw), sizes(128, **kw)):
             assert a <= 1.07 * b, (kw, a, b)
+
+
+def test_host_tensors_are_refused(monkeypatch):
+    """The layer's wrappers on tensors in host memory never reach the library."""
+    import torch
+
+    from paper_2511_07343_amd import inputs
+
+    def reached(*a, **kw):
+        raise AssertionError("the library was called")
+
+    for n in ("tnt_mem_fwd", "tnt_mem_bwd", "tnt_mem_step", "tnt_mem_state_init"):
+        monkeypatch.setattr(tnt, n, reached)
+    cfg = inputs.WORKLOADS[0]
+    x = tnt.device_inputs(inputs.make_inputs(cfg, 0), cfg, device="cpu")
+    for stream in (None, 0):
+        for call in (lambda: tnt.forward(cfg, x, stream=stream), lambda: tnt.backward(cfg, x, x["dO"], stream=stream),
+                     lambda: tnt.step_forward(cfg, x, [8], stream=stream)):
+            with pytest.raises(ValueError, match="GPU"):
+                call()
