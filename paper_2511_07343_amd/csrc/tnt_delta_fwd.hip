@@ -10,8 +10,9 @@ constexpr int AP = 68;  // floats a row of the 64x64 matrices in LDS (16-byte ro
 // ---------------------------------------------------------------------------------
 // Packed sequences: seq_start [nseq + 1] on the device -> the first chunk slot of every
 // sequence and the table of slots.  One workgroup, a thread a sequence: a scan of the chunk
-// counts, then each thread writes its sequence's slots in turn.  Starts are clamped into
-// [0, L] and made non-decreasing, so that no list of starts leads outside the tensors.
+// counts, then each thread writes its sequence's slots in turn.  A launch, and 64 ns a chunk of
+// the longest sequence, whose chain takes over 1 us of each.  Starts are clamped into [0, L]
+// and made non-decreasing, so that no list of starts leads outside the tensors.
 // ---------------------------------------------------------------------------------
 __global__ __launch_bounds__(1024) void delta_plan_kernel(const int* start, int nseq, int L, int slots,
                                                           int* first, int4* table) {
